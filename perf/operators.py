@@ -1,0 +1,424 @@
+"""The dense half of a layer as cases to be timed: layer norm forward and backward, products of matrices held in 4 bits (MX blocks: 32 values that
+share a power of two), and the orthogonalised update of weights.  Sizes are those of the layers that the package's partitions stand for (rows = the
+nodes of a partition, columns = feature or hidden widths) and generic square-ish ones.
+
+`run` computes a case in its plain form, elementary torch operations in 32 bits, or (own = True) by the package's calls.  `exact` computes the
+definitions in 64 bits, written apart from the plain form.
+"""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda:0"
+EPS = 1e-5                              # of the layer norm
+NORM_EPS = 1e-7                         # added to an update's norm
+STEPS = ((3.4445, -4.7750, 2.0315),) * 5
+RANDOM_TAG = 0x4D583443                 # last counter word of the numbers that round an MX matrix
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _case(kind, name=None, **sizes):
+    case = dict(kind=kind, **sizes)
+    if name is not None:
+        case["name"] = name
+    return case
+
+
+def listed():
+    return [
+        # The smallest partition in use, a narrow hidden layer: a few microseconds, what counts is the call.
+        _case("norm forward", "norm forward tiny", rows=2_000, dim=128, type="f32", pad=True),
+        # One of four parts of a graph with 602 input features, rows padded to whole lines.
+        _case("norm forward", "norm forward 602", rows=58_000, dim=602, type="f32", pad=True),
+        # One of eight parts of a 2.45M-node graph, hidden layer of a training step.
+        _case("norm backward", "norm backward hidden", rows=306_000, dim=256, type="f32", pad=True),
+        # Unpadded rows of an odd width in 16 bits: no row but the first begins on a line.
+        _case("norm backward", "norm backward ragged", rows=24_000, dim=301, type="bf16", pad=False),
+        # A layer's product in a forward pass: the features are quantised and multiplied with weights kept in 4 bits.
+        _case("linear forward", "linear forward 602", rows=58_000, k=602, n=256, type="f32"),
+        # Its gradients in a backward pass: the output's gradient is quantised both ways, stochastically, and gives the input's and the weight's.
+        _case("linear backward", "linear backward 300", rows=196_000, k=300, n=256, type="f32"),
+        # A few nodes asked for at a time, wide layer, both operands kept in 4 bits: latency and the reading of the weights.
+        _case("product", "product few rows", rows=5, k=4_096, n=8_192, type="bf16"),
+        # The same layer over many rows: bound by the matrix cores.
+        _case("product", "product large", rows=8_192, k=4_096, n=8_192, type="f32"),
+        # Rows kept in 4 bits between two uses: written with stochastic rounding, read back.
+        _case("round trip", "round trip 300", rows=179_000, k=300, type="bf16"),
+        # The hidden layers' weights, updated together.
+        _case("update", "update hidden", count=3, rows=256, cols=256, type="f32"),
+        # An input layer's weights, tall, in 16 bits.
+        _case("update", "update input", count=1, rows=602, cols=256, type="bf16"),
+        # A wide layer's weights: bound by the matrix cores.
+        _case("update", "update wide", count=1, rows=2_048, cols=4_096, type="f32"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["norm forward", "norm backward", "linear forward", "linear backward", "product", "round trip", "update"])
+    kind_of_type = rng.choice(["f32", "bf16"])
+    if kind == "update":
+        rows, cols, count = _log(rng, 16, 4_096), _log(rng, 16, 2_048), rng.randint(1, 4)
+        while rows * cols * min(rows, cols) * count > 2_048 * 2_048 * 4_096:
+            count, rows = max(1, count // 2), rows // 2 if count == 1 else rows
+        return _case(kind, count=count, rows=rows, cols=cols, type=kind_of_type)
+    width = _log(rng, 16, 2_048)
+    if rng.random() < 0.5:
+        width = max(8, width // 8 * 8)
+    if kind.startswith("norm"):
+        rows = min(_log(rng, 1, 306_000), 306_000 * 256 // width)
+        return _case(kind, rows=rows, dim=width, type=kind_of_type, pad=rng.random() < 0.5)
+    if kind == "round trip":
+        return _case(kind, rows=min(_log(rng, 16, 306_000), 306_000 * 256 // width), k=width, type=kind_of_type)
+    n = _log(rng, 16, 2_048)
+    rows = _log(rng, 16, 306_000) if kind != "product" else _log(rng, 1, 306_000)
+    rows = max(1, min(rows, 306_000 * 256 // max(width, n), 8_192 * 4_096 * 8_192 // (width * n)))
+    return _case(kind, rows=rows, k=width, n=n, type=kind_of_type)
+
+
+# ---- inputs ------------------------------------------------------------------------------------------------------------------------
+
+def _padded(rows, dim, dtype, pad):
+    """An uninitialised matrix whose rows cover whole 128-byte lines if `pad`."""
+    line = 128 // dtype.itemsize
+    return torch.empty(rows, -(-dim // line) * line if pad else dim, dtype=dtype, device=DEV)[:, :dim]
+
+
+def _fill(gen, rows, dim, dtype, pad, scale=1.0, shift=0.0):
+    x = _padded(rows, dim, dtype, pad)
+    x.copy_(torch.randn(rows, dim, generator=gen, device=DEV).mul_(scale).add_(shift))
+    return x
+
+
+def _gradient(gen, rows, dim, dtype):
+    """Gradients of nodes: of a few the loss knows nothing."""
+    g = torch.randn(rows, dim, generator=gen, device=DEV) * 1e-3
+    g *= torch.rand(rows, 1, generator=gen, device=DEV) > 0.05
+    return g.to(dtype)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    dtype, kind = TYPES[case["type"]], case["kind"]
+    state = dict(case=dict(case), dtype=dtype, kept={})
+    if kind.startswith("norm"):
+        rows, dim = case["rows"], case["dim"]
+        state["x"] = _fill(gen, rows, dim, dtype, case["pad"], 1.5, 0.25)
+        state["gamma"] = 1 + 0.1 * torch.randn(dim, generator=gen, device=DEV)
+        state["beta"] = 0.1 * torch.randn(dim, generator=gen, device=DEV)
+        if kind == "norm backward":
+            state["dy"] = _fill(gen, rows, dim, dtype, case["pad"], 1e-3)
+            x = state["x"].double()
+            mean = x.mean(1)
+            state["stats"] = torch.stack([mean, ((x - mean[:, None]).square().mean(1) + EPS).rsqrt()], 1).float()
+    elif kind == "linear forward":
+        state["x"] = torch.randn(case["rows"], case["k"], generator=gen, device=DEV).to(dtype)
+        state["w"] = _quantize(torch.randn(case["n"], case["k"], generator=gen, device=DEV) / math.sqrt(case["k"]))
+    elif kind == "linear backward":
+        state["dz"] = _gradient(gen, case["rows"], case["n"], dtype)
+        state["wt"] = _quantize((torch.randn(case["n"], case["k"], generator=gen, device=DEV) / math.sqrt(case["k"])).t())
+        state["xt"] = _quantize(torch.randn(case["rows"], case["k"], generator=gen, device=DEV).relu_().t())
+        state["seed"] = seed * 2_654_435_761 + 97
+    elif kind == "product":
+        state["a"] = _quantize(torch.randn(case["rows"], case["k"], generator=gen, device=DEV))
+        state["b"] = _quantize(torch.randn(case["n"], case["k"], generator=gen, device=DEV) / math.sqrt(case["k"]))
+    elif kind == "round trip":
+        state["x"] = torch.randn(case["rows"], case["k"], generator=gen, device=DEV).to(dtype)
+        state["seed"] = seed * 2_654_435_761 + 97
+    else:
+        count, rows, cols = case["count"], case["rows"], case["cols"]
+        rank = min(rows, cols)
+        left = torch.randn(count, rows, rank, generator=gen, device=DEV) / torch.arange(1, rank + 1, device=DEV)
+        right = torch.randn(count, rank, cols, generator=gen, device=DEV)
+        state["g"] = ((left @ right + 0.05 * torch.randn(count, rows, cols, generator=gen, device=DEV)) * 1e-3).to(dtype)
+    return state
+
+
+# ---- the plain forms -----------------------------------------------------------------------------------------------------------------
+# An MX matrix of r rows and c columns: codes [r, 64 ceil(c / 128)], two of 4 bits to a byte, the even column's low; scales [ceil(c / 128), r, 4],
+# one byte for 32 columns, the exponent of a power of two plus 127.  What lies beyond column c has code 0.
+
+_GRID = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _random16(rows, columns, seed):
+    """[rows, columns] integers below 2^16 (columns a multiple of 8): Philox4x32-10, counter (column / 8, row low, row high, tag), key = seed."""
+    low = 0xFFFFFFFF
+    c0 = torch.arange(columns // 8, device=DEV).expand(rows, -1)
+    c1 = torch.arange(rows, device=DEV)[:, None].expand(-1, columns // 8)
+    c2, c3 = torch.zeros_like(c0), torch.full_like(c0, RANDOM_TAG)
+    k0, k1 = seed & low, (seed >> 32) & low
+    for _ in range(10):
+        a, b = c0 * 0xD2511F53, c2 * 0xCD9E8D57
+        c0, c1, c2, c3 = ((b >> 32) & low) ^ c1 ^ k0, b & low, ((a >> 32) & low) ^ c3 ^ k1, a & low
+        k0, k1 = (k0 + 0x9E3779B9) & low, (k1 + 0xBB67AE85) & low
+    words = torch.stack([c0, c1, c2, c3], -1)
+    return torch.stack([words & 0xFFFF, words >> 16], -1).reshape(rows, columns)
+
+
+def _quantize(x, seed=None):
+    """(codes, scales) of a matrix, rounded to nearest or (seed) stochastically."""
+    rows, cols = x.shape
+    padded = torch.nn.functional.pad(x.float(), (0, -cols % 128)).contiguous()
+    bits = padded.reshape(rows, -1, 32).abs().amax(2).view(torch.int32)
+    field = bits >> 23
+    byte = (field - 2 if seed is None else field - 2 + ((bits & 0x7FFFFF) > 0x400000).int()).clamp_(min=0)
+    y = padded.abs().reshape(rows, -1, 32) * ((254 - byte) << 23).view(torch.float32)[:, :, None]
+    y = y.reshape(rows, -1)
+    step = torch.where(y < 2, 0.5, torch.where(y < 4, 1.0, 2.0))
+    base = torch.where(y < 2, 0, torch.where(y < 4, 2, 4))
+    if seed is None:
+        code = (y / step).round().int() + base
+    else:
+        code = (((y / step) * 65536).to(torch.int64) + _random16(rows, y.shape[1], seed) >> 16).int() + base
+    code = code.clamp_(max=7) | torch.signbit(padded).int() << 3
+    code = code.reshape(rows, -1, 2)
+    codes = (code[..., 0] | code[..., 1] << 4).to(torch.uint8)
+    return codes, byte.to(torch.uint8).reshape(rows, -1, 4).transpose(0, 1).contiguous()
+
+
+def _dequantize(packed, cols):
+    codes, scales = packed
+    code = torch.stack([codes & 15, codes >> 4], -1).reshape(codes.shape[0], -1, 32).int()
+    value = torch.tensor(_GRID + tuple(-v for v in _GRID), device=DEV)[code]
+    byte = scales.transpose(0, 1).reshape(codes.shape[0], -1).int()
+    scale = torch.where(byte == 0, 0x400000, byte << 23).view(torch.float32)
+    return (value * scale[:, :, None]).reshape(codes.shape[0], -1)[:, :cols]
+
+
+def _orthogonalized(g):
+    x = g.float()
+    tall = x.shape[1] > x.shape[2]
+    if tall:
+        x = x.transpose(1, 2).contiguous()
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + NORM_EPS)
+    for a, b, c in STEPS:
+        square = x @ x.transpose(1, 2)
+        x = a * x + (b * square + c * (square @ square)) @ x
+    return x.transpose(1, 2) if tall else x
+
+
+def _plain(state):
+    case, dtype, kind = state["case"], state["dtype"], state["case"]["kind"]
+    if kind == "norm forward":
+        x = state["x"].float()
+        mean = x.mean(1, keepdim=True)
+        centred = x - mean
+        rstd = (centred.square().mean(1, keepdim=True) + EPS).rsqrt()
+        return dict(y=(centred * rstd * state["gamma"] + state["beta"]).to(dtype), stats=torch.cat([mean, rstd], 1))
+    if kind == "norm backward":
+        dy = state["dy"].float()
+        mean, rstd = state["stats"][:, :1], state["stats"][:, 1:]
+        normed = (state["x"].float() - mean) * rstd
+        g = dy * state["gamma"]
+        dx = rstd * (g - g.mean(1, keepdim=True) - normed * (g * normed).mean(1, keepdim=True))
+        return dict(dx=dx.to(dtype), dgamma=(dy * normed).sum(0), dbeta=dy.sum(0))
+    if kind == "linear forward":
+        x = _dequantize(_quantize(state["x"]), case["k"])
+        return (x @ _dequantize(state["w"], case["k"]).t()).to(dtype)
+    if kind == "linear backward":
+        dz = state["dz"]
+        rows = _dequantize(_quantize(dz, state["seed"]), case["n"])
+        columns = _dequantize(_quantize(dz.t(), state["seed"] + 1), case["rows"])
+        return dict(dx=(rows @ _dequantize(state["wt"], case["n"]).t()).to(dtype), dw=columns @ _dequantize(state["xt"], case["rows"]).t())
+    if kind == "product":
+        return (_dequantize(state["a"], case["k"]) @ _dequantize(state["b"], case["k"]).t()).to(dtype)
+    if kind == "round trip":
+        return _dequantize(_quantize(state["x"], state["seed"]), case["k"]).to(dtype)
+    return _orthogonalized(state["g"]).to(dtype)
+
+
+# ---- the package's calls -------------------------------------------------------------------------------------------------------------
+
+def _buffers(state, make):
+    """Outputs, workspaces and intermediate matrices, which a training program keeps from step to step."""
+    if not state["kept"]:
+        state["kept"].update(make())
+    return state["kept"]
+
+
+def _mx4(B, rows, cols):
+    return B.adaqp_mx4_empty(rows, cols, DEV)
+
+
+def _bytes(n):
+    return torch.empty(max(n, 1), dtype=torch.uint8, device=DEV)
+
+
+def _own(state):
+    from paper_2306_01381_amd import binding as B
+    case, dtype, kind = state["case"], state["dtype"], state["case"]["kind"]
+    if kind == "norm forward":
+        rows, dim = case["rows"], case["dim"]
+        kept = _buffers(state, lambda: dict(y=_padded(rows, dim, dtype, case["pad"]), stats=torch.empty(rows, 2, device=DEV)))
+        B.adaqp_layernorm_forward(state["x"], dim, state["gamma"], state["beta"], EPS, kept["y"], kept["stats"])
+        return dict(y=kept["y"], stats=kept["stats"])
+    if kind == "norm backward":
+        rows, dim = case["rows"], case["dim"]
+        kept = _buffers(state, lambda: dict(dx=_padded(rows, dim, dtype, case["pad"]), dgamma=torch.empty(dim, device=DEV), dbeta=torch.empty(dim, device=DEV),
+                                            work=_bytes(B.adaqp_layernorm_workspace_bytes(rows, dim))))
+        B.adaqp_layernorm_backward(state["x"], state["dy"], dim, state["stats"], state["gamma"], kept["dx"], kept["dgamma"], kept["dbeta"], kept["work"])
+        return dict(dx=kept["dx"], dgamma=kept["dgamma"], dbeta=kept["dbeta"])
+    if kind == "linear forward":
+        rows, k, n = case["rows"], case["k"], case["n"]
+        kept = _buffers(state, lambda: dict(x=_mx4(B, rows, k), z=torch.empty(rows, n, dtype=dtype, device=DEV),
+                                            work=_bytes(B.adaqp_mx4_matmul_workspace_bytes(rows, n, k))))
+        B.adaqp_mx4_quantize(state["x"], k, B.MX4_NEAREST, 0, kept["x"], None)
+        B.adaqp_mx4_matmul(kept["x"], state["w"], k, kept["z"], kept["work"])
+        return kept["z"]
+    if kind == "linear backward":
+        rows, k, n = case["rows"], case["k"], case["n"]
+        need = lambda: max(B.adaqp_mx4_matmul_workspace_bytes(rows, k, n), B.adaqp_mx4_matmul_workspace_bytes(n, k, rows))  # noqa: E731
+        kept = _buffers(state, lambda: dict(rows=_mx4(B, rows, n), columns=_mx4(B, n, rows), dx=torch.empty(rows, k, dtype=dtype, device=DEV),
+                                            dw=torch.empty(n, k, device=DEV), work=_bytes(need())))
+        B.adaqp_mx4_quantize(state["dz"], n, B.MX4_STOCHASTIC, state["seed"], kept["rows"], kept["columns"])
+        B.adaqp_mx4_matmul(kept["rows"], state["wt"], n, kept["dx"], kept["work"])
+        B.adaqp_mx4_matmul(kept["columns"], state["xt"], rows, kept["dw"], kept["work"])
+        return dict(dx=kept["dx"], dw=kept["dw"])
+    if kind == "product":
+        rows, k, n = case["rows"], case["k"], case["n"]
+        kept = _buffers(state, lambda: dict(out=torch.empty(rows, n, dtype=dtype, device=DEV), work=_bytes(B.adaqp_mx4_matmul_workspace_bytes(rows, n, k))))
+        B.adaqp_mx4_matmul(state["a"], state["b"], k, kept["out"], kept["work"])
+        return kept["out"]
+    if kind == "round trip":
+        rows, k = case["rows"], case["k"]
+        kept = _buffers(state, lambda: dict(x=_mx4(B, rows, k), out=torch.empty(rows, k, dtype=dtype, device=DEV)))
+        B.adaqp_mx4_quantize(state["x"], k, B.MX4_STOCHASTIC, state["seed"], kept["x"], None)
+        B.adaqp_mx4_dequantize(kept["x"], k, kept["out"])
+        return kept["out"]
+    count, rows, cols = case["count"], case["rows"], case["cols"]
+    kept = _buffers(state, lambda: dict(out=torch.empty(count, rows, cols, dtype=dtype, device=DEV),
+                                        work=_bytes(B.adaqp_orthogonalize_workspace_bytes(count, rows, cols))))
+    B.adaqp_orthogonalize(state["g"], kept["out"], STEPS, NORM_EPS, kept["work"])
+    return kept["out"]
+
+
+def run(state):
+    return _own(state) if own else _plain(state)
+
+
+# ---- what a pass cannot do without -----------------------------------------------------------------------------------------------------
+
+def work(case):
+    kind, size = case["kind"], TYPES[case["type"]].itemsize
+    packed = lambda rows, cols: rows * (cols / 2 + cols / 32)  # noqa: E731
+    if kind == "norm forward":
+        cells = case["rows"] * case["dim"]
+        return dict(bytes=2 * size * cells + 8 * case["rows"] + 8 * case["dim"], flops=8 * cells)
+    if kind == "norm backward":
+        cells = case["rows"] * case["dim"]
+        return dict(bytes=3 * size * cells + 8 * case["rows"] + 12 * case["dim"], flops=15 * cells)
+    if kind == "update":
+        count, n, m = case["count"], min(case["rows"], case["cols"]), max(case["rows"], case["cols"])
+        # the two symmetric products cost half of a product, the third all of it
+        return dict(bytes=2 * size * count * n * m, flops=len(STEPS) * count * (n * n * m + n * n * n + 2 * n * n * m))
+    rows, k = case["rows"], case["k"]
+    if kind == "round trip":
+        return dict(bytes=2 * size * rows * k, flops=10 * rows * k)
+    n = case["n"]
+    if kind == "linear forward":
+        return dict(bytes=size * rows * (k + n) + packed(n, k), flops=2 * rows * k * n)
+    if kind == "linear backward":
+        return dict(bytes=size * rows * (n + k) + packed(k, n) + packed(k, rows) + 4 * n * k, flops=4 * rows * k * n)
+    return dict(bytes=packed(rows, k) + packed(n, k) + size * rows * n, flops=2 * rows * k * n)
+
+
+# ---- the definitions in 64 bits ----------------------------------------------------------------------------------------------------------
+
+def _philox(rows, columns, seed):
+    """The numbers that _random16 gives, from the generator's definition on 64-bit words of the host."""
+    word, shift = np.uint64(0xFFFFFFFF), np.uint64(32)
+    x = [np.broadcast_to(np.arange(columns // 8, dtype=np.uint64), (rows, columns // 8)).copy(),
+         np.broadcast_to(np.arange(rows, dtype=np.uint64)[:, None], (rows, columns // 8)).copy(),
+         np.zeros((rows, columns // 8), np.uint64), np.full((rows, columns // 8), RANDOM_TAG, np.uint64)]
+    key = [seed % (1 << 32), (seed >> 32) % (1 << 32)]
+    for _ in range(10):
+        first, second = x[0] * np.uint64(0xD2511F53), x[2] * np.uint64(0xCD9E8D57)
+        x = [(second >> shift) ^ x[1] ^ np.uint64(key[0]), second & word, (first >> shift) ^ x[3] ^ np.uint64(key[1]), first & word]
+        key = [(key[0] + 0x9E3779B9) % (1 << 32), (key[1] + 0xBB67AE85) % (1 << 32)]
+    out = np.empty((rows, columns // 8, 8), np.int64)
+    for j in range(8):
+        out[:, :, j] = (x[j // 2] >> np.uint64(16 * (j % 2))) & np.uint64(0xFFFF)
+    return torch.from_numpy(out.reshape(rows, columns)).to(DEV)
+
+
+def _exact_mx4(x, seed=None):
+    """The values that a matrix's 4-bit form stands for: each block of 32 in units of 2^e, where e comes from the block's largest magnitude."""
+    rows, cols = x.shape
+    full = torch.zeros(rows, -(-cols // 32) * 32, dtype=torch.float64, device=DEV)
+    full[:, :cols] = x
+    block = full.reshape(rows, -1, 32)
+    most = block.abs().amax(2, keepdim=True)
+    fraction, exponent = torch.frexp(most)                       # most = fraction 2^exponent, fraction in [1/2, 1)
+    e = exponent.double() - 3
+    if seed is not None:
+        e = e + (fraction > 0.75)
+    e = torch.where(most == 0, -127.0, e.clamp(min=-127))
+    y = block.abs() / torch.exp2(e)
+    if seed is None:
+        # midpoints, the even neighbour's side wins a tie
+        up = sum((y >= t).double() * s if even_above else (y > t).double() * s
+                 for t, s, even_above in ((0.25, 0.5, False), (0.75, 0.5, True), (1.25, 0.5, False), (1.75, 0.5, True), (2.5, 1.0, False), (3.5, 1.0, True), (5.0, 2.0, False)))
+    else:
+        grid = torch.tensor(_GRID, dtype=torch.float64, device=DEV)
+        at = torch.searchsorted(grid, y.contiguous(), right=True) - 1
+        below, above = grid[at], grid[(at + 1).clamp(max=7)]
+        share = torch.where(above > below, (y - below) / (above - below).clamp(min=0.5), 0.0)
+        wide = -(-cols // 128) * 128
+        r = _philox(rows, wide, seed)[:, :full.shape[1]].reshape(y.shape)
+        up = torch.where(torch.floor(share * 65536) + r >= 65536, above, below)
+    return (torch.sign(block) * up * torch.exp2(e)).reshape(rows, -1)[:, :cols]
+
+
+def _exact_kept(packed, cols):
+    codes, scales = (t.cpu().numpy() for t in packed)
+    values = np.array(_GRID + tuple(-v for v in _GRID))
+    out = np.empty((codes.shape[0], 2 * codes.shape[1]))
+    out[:, 0::2], out[:, 1::2] = values[codes % 16], values[codes // 16]
+    e = scales.transpose(1, 0, 2).reshape(codes.shape[0], -1).astype(np.float64) - 127
+    return torch.from_numpy((out.reshape(codes.shape[0], -1, 32) * np.exp2(e)[:, :, None]).reshape(codes.shape[0], -1)[:, :cols].copy()).to(DEV)
+
+
+def exact(case, seed):
+    state, kind = prepare(case, seed), case["kind"]
+    if kind == "norm forward":
+        x, n = state["x"].double(), case["dim"]
+        mean = x.sum(1) / n
+        var = ((x * x).sum(1) / n - mean * mean).clamp(min=0)
+        rstd = 1 / torch.sqrt(var + EPS)
+        y = (x - mean[:, None]) * (rstd[:, None] * state["gamma"].double()[None]) + state["beta"].double()[None]
+        return dict(y=y, stats=torch.stack([mean, rstd], 1))
+    if kind == "norm backward":
+        x, dy, n = state["x"].double(), state["dy"].double(), case["dim"]
+        mean, rstd = state["stats"].double().unbind(1)
+        h = (x - mean[:, None]) * rstd[:, None]
+        g = dy * state["gamma"].double()[None]
+        first, second = g.sum(1) / n, (g * h).sum(1) / n
+        return dict(dx=(g - (first[:, None] + h * second[:, None])) * rstd[:, None], dgamma=(dy * h).sum(0), dbeta=dy.sum(0))
+    if kind == "linear forward":
+        return _exact_mx4(state["x"]) @ _exact_kept(state["w"], case["k"]).t()
+    if kind == "linear backward":
+        rows = _exact_mx4(state["dz"], state["seed"])
+        columns = _exact_mx4(state["dz"].t(), state["seed"] + 1)
+        return dict(dx=rows @ _exact_kept(state["wt"], case["n"]).t(), dw=columns @ _exact_kept(state["xt"], case["rows"]).t())
+    if kind == "product":
+        return _exact_kept(state["a"], case["k"]) @ _exact_kept(state["b"], case["k"]).t()
+    if kind == "round trip":
+        return _exact_mx4(state["x"], state["seed"])
+    out = []
+    for g in state["g"].double().unbind(0):
+        flip = g.shape[0] > g.shape[1]
+        x = (g.t() if flip else g) / (torch.linalg.norm(g) + NORM_EPS)
+        for a, b, c in STEPS:
+            gram = x @ x.t()
+            x = a * x + b * (gram @ x) + c * (gram @ (gram @ x))
+        out.append(x.t() if flip else x)
+    return torch.stack(out)
