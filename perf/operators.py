@@ -245,10 +245,6 @@ def _buffers(state, make):
     return state["kept"]
 
 
-def _mx4(B, rows, cols):
-    return B.adaqp_mx4_empty(rows, cols, DEV)
-
-
 def _bytes(n):
     return torch.empty(max(n, 1), dtype=torch.uint8, device=DEV)
 
@@ -269,7 +265,7 @@ def _own(state):
         return dict(dx=kept["dx"], dgamma=kept["dgamma"], dbeta=kept["dbeta"])
     if kind == "linear forward":
         rows, k, n = case["rows"], case["k"], case["n"]
-        kept = _buffers(state, lambda: dict(x=_mx4(B, rows, k), z=torch.empty(rows, n, dtype=dtype, device=DEV),
+        kept = _buffers(state, lambda: dict(x=B.mx4_empty(rows, k, DEV), z=torch.empty(rows, n, dtype=dtype, device=DEV),
                                             work=_bytes(B.adaqp_mx4_matmul_workspace_bytes(rows, n, k))))
         B.adaqp_mx4_quantize(state["x"], k, B.MX4_NEAREST, 0, kept["x"], None)
         B.adaqp_mx4_matmul(kept["x"], state["w"], k, kept["z"], kept["work"])
@@ -277,7 +273,7 @@ def _own(state):
     if kind == "linear backward":
         rows, k, n = case["rows"], case["k"], case["n"]
         need = lambda: max(B.adaqp_mx4_matmul_workspace_bytes(rows, k, n), B.adaqp_mx4_matmul_workspace_bytes(n, k, rows))  # noqa: E731
-        kept = _buffers(state, lambda: dict(rows=_mx4(B, rows, n), columns=_mx4(B, n, rows), dx=torch.empty(rows, k, dtype=dtype, device=DEV),
+        kept = _buffers(state, lambda: dict(rows=B.mx4_empty(rows, n, DEV), columns=B.mx4_empty(n, rows, DEV), dx=torch.empty(rows, k, dtype=dtype, device=DEV),
                                             dw=torch.empty(n, k, device=DEV), work=_bytes(need())))
         B.adaqp_mx4_quantize(state["dz"], n, B.MX4_STOCHASTIC, state["seed"], kept["rows"], kept["columns"])
         B.adaqp_mx4_matmul(kept["rows"], state["wt"], n, kept["dx"], kept["work"])
@@ -290,7 +286,7 @@ def _own(state):
         return kept["out"]
     if kind == "round trip":
         rows, k = case["rows"], case["k"]
-        kept = _buffers(state, lambda: dict(x=_mx4(B, rows, k), out=torch.empty(rows, k, dtype=dtype, device=DEV)))
+        kept = _buffers(state, lambda: dict(x=B.mx4_empty(rows, k, DEV), out=torch.empty(rows, k, dtype=dtype, device=DEV)))
         B.adaqp_mx4_quantize(state["x"], k, B.MX4_STOCHASTIC, state["seed"], kept["x"], None)
         B.adaqp_mx4_dequantize(kept["x"], k, kept["out"])
         return kept["out"]
