@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libadaqp.so (include/adaqp.h).  Argument marshalling only.
+"""Thin ctypes binding of libadaqp.so (include/adaqp.h, include/adaqp_dense.h).  Argument marshalling only.
 
 Every function has the name of the C entry point it calls.  Tensors are torch tensors that already live
 where the C function expects them (device tensors for *_dev arguments, numpy arrays for the host-only
@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libadaqp.so")
 OK, EINVAL, EBITS, ESIZE, EHIP = 0, -1, -2, -3, -4
 SERIAL, ISOLATED, FREE, CHAIN = 0, 1, 2, 3
 FORWARD, BACKWARD = 0, 1
+MX4_NEAREST, MX4_STOCHASTIC = 0, 1
 
 _i64, _i32, _u64, _vp = ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_void_p
 
@@ -165,6 +166,17 @@ _SIGNATURES = {
     "adaqp_probe_stream": (ctypes.c_int, [_vp, _vp, _i64, _i32, _vp]),
     "adaqp_probe_xcd_of_workgroup": (ctypes.c_int, [_vp, _i32, _vp]),
     "adaqp_layer_desc_bytes": (_i64, []),
+    "adaqp_layernorm_forward": (ctypes.c_int, [_vp, _i64, _i64, _i32, _i32, _vp, _vp, ctypes.c_float, _vp, _i64, _vp, _vp]),
+    "adaqp_layernorm_workspace_bytes": (ctypes.c_int, [_i64, _i32, ctypes.POINTER(_i64)]),
+    "adaqp_layernorm_backward": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _i64, _vp]),
+    "adaqp_mx4_code_bytes": (_i64, [_i64, _i64]),
+    "adaqp_mx4_scale_bytes": (_i64, [_i64, _i64]),
+    "adaqp_mx4_quantize": (ctypes.c_int, [_vp, _i64, _i64, _i64, _i32, _i32, _u64, _vp, _vp, _vp, _vp, _vp]),
+    "adaqp_mx4_dequantize": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _i64, _i32, _vp]),
+    "adaqp_mx4_matmul_workspace_bytes": (ctypes.c_int, [_i64, _i64, _i64, ctypes.POINTER(_i64)]),
+    "adaqp_mx4_matmul": (ctypes.c_int, [_vp, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _i32, _vp, _i64, _vp]),
+    "adaqp_orthogonalize_workspace_bytes": (ctypes.c_int, [_i32, _i64, _i64, ctypes.POINTER(_i64)]),
+    "adaqp_orthogonalize": (ctypes.c_int, [_vp, _i64, _i64, _vp, _i64, _i64, _i32, _i64, _i64, _i32, _i32, _vp, ctypes.c_float, _vp, _i64, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -899,3 +911,143 @@ def adaqp_probe_xcd_of_workgroup(n_workgroups: int, device="cuda:0",
     _check(lib().adaqp_probe_xcd_of_workgroup(out.data_ptr(), n_workgroups, _stream(stream)),
            "adaqp_probe_xcd_of_workgroup")
     return out[:n_workgroups]
+
+
+# ---- adaqp_dense.h -----------------------------------------------------------------------------------------------------------------------
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+def _elements(t: torch.Tensor, dim: int, name: str) -> Tuple[int, int, int, int]:
+    """(pointer, rows, leading dimension, type) of a 2-D fp32 or bf16 device tensor whose rows are contiguous and hold `dim` columns."""
+    if not t.is_cuda or t.dtype not in _TYPES or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise TypeError(f"{name} must be a 2-D fp32 or bf16 device tensor with unit column stride")
+    if t.shape[1] < dim:
+        raise ValueError(f"{name} has {t.shape[1]} columns, {dim} are wanted")
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    return t.data_ptr(), t.shape[0], ld, _TYPES[t.dtype]
+
+
+def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+    p = _dev(t, torch.float32, name)
+    if t is not None and t.numel() < n:
+        raise ValueError(f"{name} has {t.numel()} elements, {n} are wanted")
+    return p
+
+
+def _workspace(t: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
+    return _dev(t, torch.uint8, "workspace"), 0 if t is None else t.numel()
+
+
+def _same(name: str, *values) -> None:
+    if len(set(values)) > 1:
+        raise ValueError(f"{name}: the tensors differ in rows or type")
+
+
+def _count(name: str, *args) -> int:
+    n = _i64()
+    _check(getattr(lib(), name)(*args, ctypes.byref(n)), name)
+    return n.value
+
+
+def adaqp_layernorm_forward(x: torch.Tensor, dim: int, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,
+                            stats: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    xp, rows, ldx, kind = _elements(x, dim, "x")
+    yp, rows_y, ldy, kind_y = _elements(y, dim, "y")
+    _same("adaqp_layernorm_forward", (rows, kind), (rows_y, kind_y))
+    _check(lib().adaqp_layernorm_forward(xp, ldx, rows, dim, kind, _vector(gamma, dim, "gamma"), _vector(beta, dim, "beta"), eps, yp, ldy,
+                                         _vector(stats, 2 * rows, "stats"), _stream(stream)), "adaqp_layernorm_forward")
+
+
+def adaqp_layernorm_workspace_bytes(n_rows: int, dim: int) -> int:
+    return _count("adaqp_layernorm_workspace_bytes", n_rows, dim)
+
+
+def adaqp_layernorm_backward(x: torch.Tensor, dy: torch.Tensor, dim: int, stats: torch.Tensor, gamma: Optional[torch.Tensor], dx: Optional[torch.Tensor],
+                             dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor], workspace: Optional[torch.Tensor],
+                             stream: Optional[torch.cuda.Stream] = None) -> None:
+    xp, rows, ldx, kind = _elements(x, dim, "x")
+    dyp, rows_dy, lddy, kind_dy = _elements(dy, dim, "dy")
+    dxp, rows_dx, lddx, kind_dx = (None, rows, 0, kind) if dx is None else _elements(dx, dim, "dx")
+    _same("adaqp_layernorm_backward", (rows, kind), (rows_dy, kind_dy), (rows_dx, kind_dx))
+    _check(lib().adaqp_layernorm_backward(xp, ldx, dyp, lddy, rows, dim, kind, _vector(stats, 2 * rows, "stats"), _vector(gamma, dim, "gamma"), dxp, lddx,
+                                          _vector(dgamma, dim, "dgamma"), _vector(dbeta, dim, "dbeta"), *_workspace(workspace), _stream(stream)),
+           "adaqp_layernorm_backward")
+
+
+def adaqp_mx4_code_bytes(n_rows: int, n_cols: int) -> int:
+    return int(lib().adaqp_mx4_code_bytes(n_rows, n_cols))
+
+
+def adaqp_mx4_scale_bytes(n_rows: int, n_cols: int) -> int:
+    return int(lib().adaqp_mx4_scale_bytes(n_rows, n_cols))
+
+
+def mx4_empty(n_rows: int, n_cols: int, device="cuda:0") -> Tuple[torch.Tensor, torch.Tensor]:
+    """Uninitialised codes [n_rows, 64 ceil(n_cols / 128)] and scales [ceil(n_cols / 128), n_rows, 4] of an MX matrix."""
+    chunks = -(-n_cols // 128)
+    return (torch.empty(n_rows, 64 * chunks, dtype=torch.uint8, device=device), torch.empty(chunks, n_rows, 4, dtype=torch.uint8, device=device))
+
+
+def _mx4(packed: Optional[Tuple[torch.Tensor, torch.Tensor]], n_rows: Optional[int], n_cols: int, name: str):
+    """(codes pointer, scales pointer, rows) of an MX matrix of n_cols columns."""
+    if packed is None:
+        return None, None, n_rows
+    codes, scales = packed
+    rows = codes.shape[0] if n_rows is None else n_rows
+    cp, sp = _dev(codes, torch.uint8, f"{name} codes"), _dev(scales, torch.uint8, f"{name} scales")
+    if tuple(codes.shape) != (rows, 64 * -(-n_cols // 128)) or tuple(scales.shape) != (-(-n_cols // 128), rows, 4):
+        raise ValueError(f"{name}: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} are not those of {rows} rows and {n_cols} columns")
+    return cp, sp, rows
+
+
+def adaqp_mx4_quantize(x: torch.Tensor, n_cols: int, rounding: int, seed: int, packed: Optional[Tuple[torch.Tensor, torch.Tensor]],
+                       packed_t: Optional[Tuple[torch.Tensor, torch.Tensor]], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """packed, packed_t: (codes, scales) of the matrix and of its transpose, as mx4_empty makes them."""
+    xp, rows, ld, kind = _elements(x, n_cols, "x")
+    cp, sp, _ = _mx4(packed, rows, n_cols, "packed")
+    ctp, stp, _ = _mx4(packed_t, n_cols, rows, "packed_t")
+    _check(lib().adaqp_mx4_quantize(xp, ld, rows, n_cols, kind, rounding, seed & (2**64 - 1), cp, sp, ctp, stp, _stream(stream)), "adaqp_mx4_quantize")
+
+
+def adaqp_mx4_dequantize(packed: Tuple[torch.Tensor, torch.Tensor], n_cols: int, x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    xp, rows, ld, kind = _elements(x, n_cols, "x")
+    cp, sp, _ = _mx4(packed, rows, n_cols, "packed")
+    _check(lib().adaqp_mx4_dequantize(cp, sp, rows, n_cols, xp, ld, kind, _stream(stream)), "adaqp_mx4_dequantize")
+
+
+def adaqp_mx4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return _count("adaqp_mx4_matmul_workspace_bytes", m, n, k)
+
+
+def adaqp_mx4_matmul(a: Tuple[torch.Tensor, torch.Tensor], b: Tuple[torch.Tensor, torch.Tensor], k: int, out: torch.Tensor,
+                     workspace: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out = a b^T for MX matrices of k columns."""
+    ac, asc, m = _mx4(a, None, k, "a")
+    bc, bsc, n = _mx4(b, None, k, "b")
+    op, rows, ldo, kind = _elements(out, n, "out")
+    if rows != m:
+        raise ValueError(f"out has {rows} rows, a {m}")
+    _check(lib().adaqp_mx4_matmul(ac, asc, m, bc, bsc, n, k, op, ldo, kind, *_workspace(workspace), _stream(stream)), "adaqp_mx4_matmul")
+
+
+def adaqp_orthogonalize_workspace_bytes(n_matrices: int, n_rows: int, n_cols: int) -> int:
+    return _count("adaqp_orthogonalize_workspace_bytes", n_matrices, n_rows, n_cols)
+
+
+def adaqp_orthogonalize(g: torch.Tensor, out: torch.Tensor, coefficients, eps: float, workspace: Optional[torch.Tensor],
+                        stream: Optional[torch.cuda.Stream] = None) -> None:
+    """g, out: [rows, cols] or [matrices, rows, cols].  coefficients: (a, b, c) of each step."""
+    g, out = (t.unsqueeze(0) if t.dim() == 2 else t for t in (g, out))
+    for t, name in ((g, "g"), (out, "out")):
+        if not t.is_cuda or t.dtype not in _TYPES or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
+            raise TypeError(f"{name} must be a 2-D or 3-D fp32 or bf16 device tensor with unit column stride")
+    _same("adaqp_orthogonalize", (g.shape, g.dtype), (out.shape, out.dtype))
+    count, rows, cols = g.shape
+    coef = np.ascontiguousarray(coefficients, dtype=np.float32).reshape(-1, 3)
+
+    def strides(t):
+        ld = t.stride(1) if rows > 1 else max(t.stride(1), cols)
+        return ld, t.stride(0) if count > 1 else max(t.stride(0), rows * ld)
+    _check(lib().adaqp_orthogonalize(g.data_ptr(), *strides(g), out.data_ptr(), *strides(out), count, rows, cols, _TYPES[g.dtype], coef.shape[0],
+                                     coef.ctypes.data, eps, *_workspace(workspace), _stream(stream)), "adaqp_orthogonalize")

@@ -1,0 +1,143 @@
+"""CPU-only checks of the dense operators: sizes, refusals before any launch, and pins of their plain definitions."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import dense as D
+from paper_2306_01381_amd import binding as B
+
+STEPS = ((3.4445, -4.7750, 2.0315),) * 5
+P = 4096                                            # stands for a device pointer: nothing here reaches a launch
+
+
+def test_mx4_sizes():
+    assert B.adaqp_mx4_code_bytes(10, 1) == 640 and B.adaqp_mx4_scale_bytes(10, 1) == 40
+    assert B.adaqp_mx4_code_bytes(3, 602) == 3 * 5 * 64 and B.adaqp_mx4_scale_bytes(3, 602) == 3 * 5 * 4
+    assert B.adaqp_mx4_code_bytes(0, 5) == 0 and B.adaqp_mx4_scale_bytes(7, 0) == 0
+    assert B.adaqp_mx4_code_bytes(-1, 5) == B.adaqp_mx4_scale_bytes(5, -1) == B.adaqp_mx4_code_bytes(1 << 31, 1) == -1
+    codes, scales = B.mx4_empty(3, 602, "cpu")
+    assert codes.numel() == B.adaqp_mx4_code_bytes(3, 602) and scales.numel() == B.adaqp_mx4_scale_bytes(3, 602)
+
+
+def test_workspaces():
+    assert B.adaqp_layernorm_workspace_bytes(0, 8) == 0
+    assert B.adaqp_layernorm_workspace_bytes(1, 8) == 256
+    assert B.adaqp_orthogonalize_workspace_bytes(0, 8, 8) == 0
+    for sizes in ((1, 1, 1), (3, 256, 256), (1, 602, 256)):
+        n = B.adaqp_orthogonalize_workspace_bytes(*sizes)
+        assert n > 0 and n % 256 == 0
+    assert B.adaqp_mx4_matmul_workspace_bytes(0, 5, 5) == 0 and B.adaqp_mx4_matmul_workspace_bytes(5, 5, 0) == 0
+    assert B.adaqp_mx4_matmul_workspace_bytes(58_000, 256, 602) % 256 == 0
+    L = B.lib()
+    n = ctypes.c_int64()
+    assert L.adaqp_layernorm_workspace_bytes(-1, 8, ctypes.byref(n)) == L.adaqp_layernorm_workspace_bytes(1, 0, ctypes.byref(n)) == B.EINVAL
+    assert L.adaqp_layernorm_workspace_bytes(1, 8, None) == L.adaqp_mx4_matmul_workspace_bytes(1, 1, 1, None) == B.EINVAL
+    assert L.adaqp_orthogonalize_workspace_bytes(1, 1, 1, None) == L.adaqp_orthogonalize_workspace_bytes(-1, 1, 1, ctypes.byref(n)) == B.EINVAL
+    assert L.adaqp_mx4_matmul_workspace_bytes(1 << 31, 1, 1, ctypes.byref(n)) == B.ESIZE
+    assert L.adaqp_orthogonalize_workspace_bytes(1, 1 << 20, 1, ctypes.byref(n)) == L.adaqp_orthogonalize_workspace_bytes(65536, 1, 1, ctypes.byref(n)) == B.ESIZE
+
+
+def _refused(name, good, changes, **kw):
+    """Each change of a good argument list is refused with its status; the good list itself is never called."""
+    fn = getattr(B.lib(), name)
+    for change, status in changes:
+        args = list(good)
+        for at, value in change.items():
+            args[at] = value
+        assert fn(*args) == status, (name, change)
+
+
+def test_layernorm_refusals():
+    forward = [P, 8, 4, 8, 0, P, P, 1e-5, P, 8, P, None]
+    _refused("adaqp_layernorm_forward", forward, [
+        ({0: None}, B.EINVAL), ({1: 7}, B.EINVAL), ({2: -1}, B.EINVAL), ({3: 0}, B.EINVAL), ({4: 2}, B.EINVAL), ({4: -1}, B.EINVAL), ({5: P + 2}, B.EINVAL),
+        ({6: P + 1}, B.EINVAL), ({7: -1.0}, B.EINVAL), ({7: float("nan")}, B.EINVAL), ({7: float("inf")}, B.EINVAL), ({8: None}, B.EINVAL), ({9: 7}, B.EINVAL),
+        ({0: P + 2}, B.EINVAL), ({8: P + 1, 4: 1}, B.EINVAL), ({9: 9}, B.EINVAL), ({10: P + 2}, B.EINVAL)])
+    assert B.lib().adaqp_layernorm_forward(None, 8, 0, 8, 0, None, None, 1e-5, None, 8, None, None) == B.OK
+    backward = [P, 8, 2 * P, 8, 4, 8, 0, P, P, 3 * P, 8, P, P, P, 1 << 20, None]
+    _refused("adaqp_layernorm_backward", backward, [
+        ({0: None}, B.EINVAL), ({1: 7}, B.EINVAL), ({2: None}, B.EINVAL), ({3: 7}, B.EINVAL), ({4: -1}, B.EINVAL), ({5: -8}, B.EINVAL), ({6: 5}, B.EINVAL),
+        ({7: None}, B.EINVAL), ({10: 7}, B.EINVAL), ({11: None}, B.EINVAL), ({12: None}, B.EINVAL), ({13: None}, B.EINVAL), ({13: P + 16}, B.EINVAL),
+        ({14: 255}, B.ESIZE), ({9: P, 10: 9}, B.EINVAL), ({9: 2 * P, 10: 9}, B.EINVAL), ({8: P + 1}, B.EINVAL)])
+    assert B.lib().adaqp_layernorm_backward(P, 8, P, 8, 0, 8, 0, None, None, None, 8, None, None, None, 0, None) == B.OK
+
+
+def test_mx4_refusals():
+    good = [P, 8, 4, 8, 0, 0, 0, P, P, P, P, None]
+    _refused("adaqp_mx4_quantize", good, [
+        ({0: None}, B.EINVAL), ({0: P + 2}, B.EINVAL), ({1: 7}, B.EINVAL), ({2: -1}, B.EINVAL), ({3: -1}, B.EINVAL), ({4: 3}, B.EINVAL), ({5: 2}, B.EINVAL),
+        ({7: None}, B.EINVAL), ({8: None}, B.EINVAL), ({9: None}, B.EINVAL), ({10: None}, B.EINVAL), ({7: P + 4}, B.EINVAL), ({10: P + 8}, B.EINVAL),
+        ({2: 1 << 31}, B.ESIZE), ({3: 1 << 31, 1: 1 << 31}, B.ESIZE)])
+    assert B.lib().adaqp_mx4_quantize(None, 0, 0, 8, 0, 0, 0, None, None, None, None, None) == B.OK
+    good = [P, P, 4, 8, P, 8, 0, None]
+    _refused("adaqp_mx4_dequantize", good, [({0: None}, B.EINVAL), ({1: None}, B.EINVAL), ({1: P + 4}, B.EINVAL), ({2: -1}, B.EINVAL), ({4: None}, B.EINVAL),
+                                            ({5: 7}, B.EINVAL), ({6: 9}, B.EINVAL), ({2: 1 << 31}, B.ESIZE)])
+    good = [P, P, 4, P, P, 8, 16, P, 8, 0, P, 1 << 20, None]
+    _refused("adaqp_mx4_matmul", good, [
+        ({0: None}, B.EINVAL), ({1: None}, B.EINVAL), ({3: None}, B.EINVAL), ({4: P + 4}, B.EINVAL), ({2: -1}, B.EINVAL), ({5: -1}, B.EINVAL), ({6: -1}, B.EINVAL),
+        ({7: None}, B.EINVAL), ({7: P + 2}, B.EINVAL), ({8: 7}, B.EINVAL), ({9: 2}, B.EINVAL), ({2: 1 << 31}, B.ESIZE), ({6: 1 << 31}, B.ESIZE)])
+    need = B.adaqp_mx4_matmul_workspace_bytes(4, 8, 100_000)
+    assert need > 0                                 # one tile: k is split
+    _refused("adaqp_mx4_matmul", good, [({6: 100_000, 11: need - 1}, B.ESIZE), ({6: 100_000, 10: None}, B.EINVAL), ({6: 100_000, 10: P + 128}, B.EINVAL)])
+
+
+def test_orthogonalize_refusals():
+    coef = np.array(STEPS, dtype=np.float32)
+    wild = np.array([[30.0, 0.0, 0.0]], dtype=np.float32)
+    broken = np.array([[np.nan, 0.0, 0.0]], dtype=np.float32)
+    good = [P, 8, 64, 2 * P, 8, 64, 2, 8, 8, 0, 5, coef.ctypes.data, 1e-7, P, 1 << 30, None]
+    _refused("adaqp_orthogonalize", good, [
+        ({0: None}, B.EINVAL), ({3: None}, B.EINVAL), ({0: P + 2}, B.EINVAL), ({1: 7}, B.EINVAL), ({4: 7}, B.EINVAL), ({2: 63}, B.EINVAL), ({5: 63}, B.EINVAL),
+        ({6: -1}, B.EINVAL), ({7: -1}, B.EINVAL), ({8: -1}, B.EINVAL), ({9: 2}, B.EINVAL), ({10: -1}, B.EINVAL), ({10: 65}, B.ESIZE), ({11: None}, B.EINVAL),
+        ({12: -1.0}, B.EINVAL), ({12: float("nan")}, B.EINVAL), ({13: None}, B.EINVAL), ({13: P + 4}, B.EINVAL), ({14: 1000}, B.ESIZE),
+        ({10: 1, 11: wild.ctypes.data}, B.EINVAL), ({10: 1, 11: broken.ctypes.data}, B.EINVAL), ({7: 1 << 20, 2: 1 << 40, 5: 1 << 40}, B.ESIZE),
+        ({3: P, 4: 9, 5: 80}, B.EINVAL)])
+    assert B.lib().adaqp_orthogonalize(None, 0, 0, None, 0, 0, 0, 8, 8, 0, 5, coef.ctypes.data, 1e-7, None, 0, None) == B.OK
+
+
+def test_random_numbers_are_those_of_the_codecs_generator(oracle):
+    seed = 0x0123456789ABCDEF
+    got = D.philox16(3, 24, seed)
+    for row in range(3):
+        for granule in range(3):
+            words = oracle.philox4x32_10([granule, row, 0, D.MX_TAG], [seed & 0xFFFFFFFF, seed >> 32])
+            want = [int(w) >> s & 0xFFFF for w in words for s in (0, 16)]
+            assert got[row, 8 * granule:8 * granule + 8].tolist() == want
+
+
+def test_mx4_definition_pins():
+    """By hand: all 16 codes at scale 1, ties, a value beyond 6, zeros, the smallest scale."""
+    v = np.concatenate([D.VALUES, -D.VALUES])
+    x = np.zeros((1, 32))
+    x[0, :16] = v
+    codes, scales = D.mx4_quantize(x)
+    assert scales.ravel().tolist() == [127, 0, 0, 0]
+    assert codes[0, :8].tolist() == [0x10, 0x32, 0x54, 0x76, 0x98, 0xBA, 0xDC, 0xFE] and not codes[0, 8:].any()
+    assert np.array_equal(D.mx4_values(codes, scales, 32), x)
+    x[0, :9] = [4, 0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 7.9]                  # ties to the even code; 7.9 to 6
+    codes, scales = D.mx4_quantize(x)
+    assert scales[0, 0, 0] == 127 and D.mx4_values(codes, scales, 9)[0].tolist() == [4, 0, 1, 1, 2, 2, 4, 4, 6]
+    codes, scales = D.mx4_quantize(np.full((1, 40), 2.0 ** -140))
+    assert scales[0, 0, :2].tolist() == [0, 0] and not (codes & 0x77).any()
+    assert D.mx4_quantize(np.array([[6.0]]), seed=1)[1][0, 0, 0] == 127 and D.mx4_quantize(np.array([[6.1]]), seed=1)[1][0, 0, 0] == 128
+
+
+def test_stochastic_rounding_is_unbiased_and_never_clips():
+    rng = np.random.default_rng(0)
+    x = rng.standard_normal((2, 64))
+    got = np.stack([D.mx4_values(*D.mx4_quantize(x, seed), 64) for seed in range(4000)])
+    step = got.max(0) - got.min(0)
+    assert np.all(np.abs(got.mean(0) - x) <= 4 * step / np.sqrt(4 * 4000) + step * 2.0 ** -16)
+    assert np.all(got.max(0) >= x) and np.all(got.min(0) <= x)
+
+
+def test_orthogonalize_definition_is_the_polynomial_of_the_singular_values():
+    rng = np.random.default_rng(1)
+    for shape in ((5, 9), (9, 5), (1, 4), (6, 6)):
+        g = rng.standard_normal(shape)
+        u, s, vt = np.linalg.svd(g, full_matrices=False)
+        s = s / np.sqrt((s * s).sum())
+        for a, b, c in STEPS:
+            s = a * s + b * s ** 3 + c * s ** 5
+        assert np.allclose(D.orthogonalize(g, STEPS, 0.0), u * s @ vt, atol=1e-12)
