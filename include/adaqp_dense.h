@@ -102,7 +102,7 @@ int adaqp_mx4_matmul_workspace_bytes(int64_t m, int64_t n, int64_t k, int64_t *b
  * Where few output tiles would leave the GPU idle, k is cut and the parts, held in the workspace in fp32, are added in order.
  * A layer's forward pass multiplies rows X with weights W (W's rows = outputs), its backward pass dZ with the MX form of W's transpose (giving
  * dX) and the transpose of dZ with the transpose of X (giving dW).
- * Errors: EINVAL, ESIZE (workspace too small; 2^31 rows or columns and more), EHIP. */
+ * Errors: EINVAL, ESIZE (workspace too small; 2^31 rows and more; more than 2^25 columns), EHIP. */
 int adaqp_mx4_matmul(const uint8_t *a_codes_dev, const uint8_t *a_scales_dev, int64_t m,
                      const uint8_t *b_codes_dev, const uint8_t *b_scales_dev, int64_t n, int64_t k,
                      void *out_dev, int64_t ldo, int32_t type, void *workspace_dev, int64_t workspace_bytes, void *stream);

@@ -60,6 +60,9 @@ __device__ __forceinline__ float lane_sum(float v)
     return v;
 }
 
+// Workgroups are dealt to the eight XCDs in turn: the place of a workgroup in a grid (a multiple of eight) such that neighbouring places share an XCD.
+__device__ __forceinline__ uint32_t xcd_neighbour(uint32_t block, uint32_t blocks) { return block % 8 * (blocks / 8) + block / 8; }
+
 inline bool valid_type(int32_t type) { return type == ADAQP_F32 || type == ADAQP_BF16; }
 
 inline int64_t element_bytes(int32_t type) { return type == ADAQP_F32 ? 4 : 2; }

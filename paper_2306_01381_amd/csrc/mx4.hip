@@ -1,9 +1,10 @@
 // MX matrices: writing them from rows, columns or both, and reading them back (adaqp_dense.h).
 //
-// A workgroup takes a tile of 128 rows and 128 columns: 16 lanes hold a row's 128 columns, 8 neighbouring ones each (a granule: one Philox call, one
-// 32-bit word of codes), 4 lanes a block.  The tile stays in registers for the rows' blocks; for the columns' blocks it goes through the LDS once
-// and a lane takes 32 rows of one column.  x is read once whichever of the two forms is wanted.  Both directions are bound by memory: 4 bytes
-// read per element of fp32 and 0.53 written per form.
+// 4 lanes hold a block of 32 columns, 8 neighbouring ones each (a granule: one Philox call, one 32-bit word of codes).  Where only the rows' form is wanted
+// the blocks of all rows are dealt out in a row, so that no lane stands for columns that do not exist.  For the columns' form a workgroup takes a tile of 128
+// columns and 64 rows through the LDS once, and a lane takes 32 rows of one column.  x is read once whichever of the two forms is wanted.  To nearest, the
+// conversions are gfx950's own, two values an instruction, and all is bound by memory: 4 bytes read per element of fp32 and 0.53 written per form.
+// Stochastically about 25 instructions per element and form, 8 of them Philox, are bound by their issue.
 #include "mx4.hpp"
 #include "philox.hpp"
 
@@ -11,14 +12,14 @@ namespace adaqp {
 namespace {
 
 constexpr uint32_t kMxTag = 0x4d583443u;
-constexpr int kTile = 128;
-constexpr int kLanes = kTile / 8;                   // of a row
-constexpr int kPasses = kTile / (kBlock / kLanes);  // a lane has one row of each
+constexpr int kLanes = kMxChunk / 8;                // of a row
+constexpr int kPassRows = kBlock / kLanes;          // a lane has one row of each pass
 
 struct MxArgs {
     const void *x;
     int64_t ld, n_rows, n_cols;
-    int64_t tiles_c;
+    uint32_t tiles_r, tiles_c;
+    uint32_t row_blocks;                            // blocks of a row that have columns
     uint64_t seed;
     uint8_t *codes, *scales, *codes_t, *scales_t;
     int64_t pitch, pitch_t;
@@ -34,31 +35,34 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t most)
     return byte < 0 ? 0 : byte;
 }
 
-// The codes of 8 values, low nibble first.  In steps of 1/2 below 2, 1 below 4, 2 beyond, the code counts the steps; all products are by powers of two.
-template <bool STOCHASTIC>
-__device__ __forceinline__ uint32_t codes_of(const float (&x)[8], uint32_t byte, const Rand128 &rnd)
+// The codes of 8 values, low nibble first.
+__device__ __forceinline__ uint32_t nearest_codes(const float (&x)[8], uint32_t byte)
 {
-    if (byte == 255) return 0;
-    const float inv = __builtin_bit_cast(float, (254u - byte) << 23);
+    const float scale = __builtin_bit_cast(float, byte << 23);  // the conversion goes by its exponent
+    uint32_t word = 0;
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[0], x[1], scale, 0);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[2], x[3], scale, 1);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[4], x[5], scale, 2);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, x[6], x[7], scale, 3);
+    return byte == 255 ? 0 : word;
+}
+
+// A value from 1 on is an fp32 number whose exponent and first fraction bit, counted from those of 1/2, are its code, and whose other 22 fraction bits are
+// the share of the way to the next one; below 2 the code counts steps of 1/2, and the share is in 16 fraction bits of the value times 2^17.
+__device__ __forceinline__ uint32_t stochastic_codes(const float (&x)[8], uint32_t byte, const Rand128 &rnd)
+{
     const uint32_t w[4] = {rnd.w0, rnd.w1, rnd.w2, rnd.w3};
+    const int power = 127 + 17 - (int)byte;
     uint32_t word = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const uint32_t bits = __builtin_bit_cast(uint32_t, x[j]);
-        const float y = __builtin_bit_cast(float, bits & 0x7FFFFFFFu) * inv;
-        const float steps = y < 2.0f ? 2.0f : y < 4.0f ? 1.0f : 0.5f;
-        const uint32_t base = y < 2.0f ? 0 : y < 4.0f ? 2 : 4;
-        uint32_t code;
-        if (STOCHASTIC) {
-            const uint32_t r = j % 2 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
-            code = (((uint32_t)(y * (steps * 65536.0f)) + r) >> 16) + base;
-        } else {
-            code = (uint32_t)rintf(y * steps) + base;
-            code = code > 7 ? 7 : code;
-        }
-        word |= (code | (bits >> 31) << 3) << (4 * j);
+        const uint32_t r = j % 2 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
+        const float z = __builtin_amdgcn_ldexpf(fabsf(x[j]), power);
+        const uint32_t low = ((uint32_t)z + r) >> 16, high = ((__builtin_bit_cast(uint32_t, z) + (r << 6)) >> 22) - ((127 + 17) * 2 - 2);
+        const uint32_t code = z < 131072.0f ? low : high;
+        word |= (code | (__builtin_bit_cast(uint32_t, x[j]) >> 28 & 8u)) << (4 * j);
     }
-    return word;
+    return byte == 255 ? 0 : word;
 }
 
 __device__ __forceinline__ Rand128 random_words(uint64_t seed, int64_t row, int64_t granule)
@@ -68,6 +72,16 @@ __device__ __forceinline__ Rand128 random_words(uint64_t seed, int64_t row, int6
 
 __device__ __forceinline__ uint32_t magnitude(float v) { return __builtin_bit_cast(uint32_t, v) & 0x7FFFFFFFu; }
 
+// The largest magnitude, NaN where there is one.
+template <int N>
+__device__ __forceinline__ float largest(const float (&x)[N])
+{
+    float most = __builtin_elementwise_maximum(fabsf(x[0]), fabsf(x[1]));
+#pragma unroll
+    for (int k = 2; k < N; k += 2) most = __builtin_elementwise_maximum(most, __builtin_elementwise_maximum(fabsf(x[k]), fabsf(x[k + 1])));
+    return most;
+}
+
 template <int PATTERN>
 __device__ __forceinline__ uint32_t moved(uint32_t v)
 {
@@ -75,40 +89,96 @@ __device__ __forceinline__ uint32_t moved(uint32_t v)
 }
 constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;       // partners of a butterfly over 16 lanes
 
-// 8 columns from col on, zeros from n_cols on.
+// 8 columns of a row from col on.  No branches, so that many such loads are under way together: what lies behind the last vector is loaded from there and set to
+// zero afterwards (keep_granule).
 template <typename T, int VW>
-__device__ __forceinline__ void load_granule(const T *row, int64_t col, int64_t n_cols, float (&x)[8])
+__device__ __forceinline__ void load_granule(const MxArgs &a, int64_t row, int64_t col, float (&x)[8])
 {
+    const T *from = (const T *)a.x + min(row, a.n_rows - 1) * a.ld;
+    const int64_t last = (a.n_cols - 1) / VW * VW;
 #pragma unroll
     for (int v = 0; v < 8; v += VW) {
         float part[VW];
-        if (col + v + VW <= n_cols) load_elements<T, VW>(row + col + v, part);
-        else for (int k = 0; k < VW; ++k) part[k] = col + v + k < n_cols ? (float)row[col + v + k] : 0.0f;
+        load_elements<T, VW>(from + min(col + v, last), part);
 #pragma unroll
         for (int k = 0; k < VW; ++k) x[v + k] = part[k];
     }
 }
 
-template <typename T, int VW, bool ROWS, bool COLS, bool STOCHASTIC>
+__device__ __forceinline__ void keep_granule(const MxArgs &a, int64_t row, int64_t col, float (&x)[8])
+{
+    const int left = row < a.n_rows ? (int)min(a.n_cols - col, (int64_t)8) : 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = k < left ? x[k] : 0.0f;
+}
+
+// The rows' form alone: blocks of 32 columns, kEach for a lane, row by row.
+template <typename T, int VW, bool STOCHASTIC>
+__global__ __launch_bounds__(kBlock) void mx4_quantize_rows_kernel(MxArgs a)
+{
+    constexpr int kEach = 2, kBlocks = kBlock / 4;
+    const uint64_t first = (uint64_t)xcd_neighbour(blockIdx.x, gridDim.x) * (kBlocks * kEach) + threadIdx.x / 4, total = (uint64_t)a.n_rows * a.row_blocks;
+    const int l = threadIdx.x % 4;
+    int64_t row[kEach];
+    uint32_t block[kEach];
+    float x[kEach][8];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        const uint64_t at = first + e * kBlocks;
+        row[e] = total >> 32 ? at / a.row_blocks : (uint32_t)at / a.row_blocks;        // at may lie behind the last: so does its row
+        block[e] = (uint32_t)(at - row[e] * a.row_blocks);
+        load_granule<T, VW>(a, row[e], block[e] * kMxBlock + l * 8, x[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        keep_granule(a, row[e], block[e] * kMxBlock + l * 8, x[e]);
+        uint32_t most = magnitude(largest<8>(x[e]));
+        most = max(most, moved<kSwap1>(most));
+        most = max(most, moved<kSwap2>(most));
+        const uint32_t byte = scale_byte<STOCHASTIC>(most);
+        const uint32_t word = STOCHASTIC ? stochastic_codes(x[e], byte, random_words(a.seed, row[e], block[e] * 4 + l)) : nearest_codes(x[e], byte);
+        if (row[e] >= a.n_rows) continue;
+        uint8_t *codes = a.codes + row[e] * a.pitch, *scales = a.scales + row[e] * 4;
+        *reinterpret_cast<uint32_t *>(codes + block[e] * 16 + l * 4) = word;
+        if (l == 0) scales[block[e] / 4 * a.n_rows * 4 + block[e] % 4] = (uint8_t)byte;
+        if (block[e] + 1 == a.row_blocks)           // the rest of the chunk
+            for (uint32_t b = block[e] + 1; b % 4 != 0; ++b) {
+                *reinterpret_cast<uint32_t *>(codes + b * 16 + l * 4) = 0;
+                if (l == 0) scales[b / 4 * a.n_rows * 4 + b % 4] = 0;
+            }
+    }
+}
+
+// The columns' form, and the rows'.
+template <typename T, int VW, bool ROWS, bool STOCHASTIC>
 __global__ __launch_bounds__(kBlock) void mx4_quantize_kernel(MxArgs a)
 {
-    __shared__ float tile[COLS ? kTile * kTile : 1];
-    const int64_t chunk_c = blockIdx.x % a.tiles_c, chunk_r = blockIdx.x / a.tiles_c;
+    constexpr int kRows = 64, kPasses = kRows / kPassRows;
+    __shared__ float tile[kRows * kMxChunk];
+    // an XCD gets neighbouring tiles, four tile rows together: their parts of the columns' lines meet in its L2
+    constexpr uint32_t kGroup = 4;
+    const uint32_t at = xcd_neighbour(blockIdx.x, gridDim.x);
+    const uint32_t group = at / (kGroup * a.tiles_c), in_group = at % (kGroup * a.tiles_c);
+    if (group * kGroup >= a.tiles_r) return;
+    const uint32_t rows = min(kGroup, a.tiles_r - group * kGroup);
+    const int64_t tile_r = group * kGroup + in_group % rows, chunk_c = in_group / rows;
+    if (chunk_c >= a.tiles_c) return;
     const int l = threadIdx.x % kLanes, r = threadIdx.x / kLanes;
     float x[kPasses][8];
-    const int64_t col = chunk_c * kTile + l * 8;
+    const int64_t col = chunk_c * kMxChunk + l * 8;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
-        const int64_t row = chunk_r * kTile + p * (kTile / kPasses) + r;
-        if (row < a.n_rows) load_granule<T, VW>((const T *)a.x + row * a.ld, col, a.n_cols, x[p]);
-        else for (int k = 0; k < 8; ++k) x[p][k] = 0.0f;
+        load_granule<T, VW>(a, tile_r * kRows + p * kPassRows + r, col, x[p]);
     }
-    if (COLS) {
-        // columns of rows 32 b .. 32 b + 31 are turned by 16 b: then the lanes of a wave, 16 columns of 4 blocks, read 64 banks
+    if ((tile_r + 1) * kRows > a.n_rows || (chunk_c + 1) * kMxChunk > a.n_cols)
+#pragma unroll
+        for (int p = 0; p < kPasses; ++p) keep_granule(a, tile_r * kRows + p * kPassRows + r, col, x[p]);
+    {
+        // rows 32 .. 63 are turned by 32 columns: then the lanes of a wave, 32 columns of both blocks, read 64 banks
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
-            const int row = p * (kTile / kPasses) + r;
-            float *to = tile + row * kTile + (l * 8 + 16 * (row / kMxBlock)) % kTile;
+            const int row = p * kPassRows + r;
+            float *to = tile + row * kMxChunk + (l * 8 + row / kMxBlock * 32) % kMxChunk;
 #pragma unroll
             for (int k = 0; k < 8; k += 4) *reinterpret_cast<float4 *>(to + k) = make_float4(x[p][k], x[p][k + 1], x[p][k + 2], x[p][k + 3]);
         }
@@ -116,16 +186,12 @@ __global__ __launch_bounds__(kBlock) void mx4_quantize_kernel(MxArgs a)
     if (ROWS) {
 #pragma unroll
         for (int p = 0; p < kPasses; ++p) {
-            const int64_t row = chunk_r * kTile + p * (kTile / kPasses) + r;
-            uint32_t most = 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) most = max(most, magnitude(x[p][k]));
+            const int64_t row = tile_r * kRows + p * kPassRows + r;
+            uint32_t most = magnitude(largest<8>(x[p]));
             most = max(most, moved<kSwap1>(most));
             most = max(most, moved<kSwap2>(most));
             const uint32_t byte = scale_byte<STOCHASTIC>(most);
-            Rand128 rnd{};
-            if (STOCHASTIC) rnd = random_words(a.seed, row, col / 8);
-            const uint32_t word = codes_of<STOCHASTIC>(x[p], byte, rnd);
+            const uint32_t word = STOCHASTIC ? stochastic_codes(x[p], byte, random_words(a.seed, row, col / 8)) : nearest_codes(x[p], byte);
             uint32_t scales = byte << (8 * (l / 4));
             scales |= moved<kMirror8>(scales);
             scales |= moved<kMirror16>(scales);
@@ -135,58 +201,51 @@ __global__ __launch_bounds__(kBlock) void mx4_quantize_kernel(MxArgs a)
             }
         }
     }
-    if (COLS) {
-        __syncthreads();
-        const int b = threadIdx.x % 4;                          // block of 32 rows
+    __syncthreads();
+    {
+        const int b = threadIdx.x % 2, c = threadIdx.x / 2;     // block of 32 rows, column
+        const int64_t row = chunk_c * kMxChunk + c;             // of the transpose
+        if (row >= a.n_cols) return;
+        const float *from = tile + b * kMxBlock * kMxChunk + (c + 32 * b) % kMxChunk;
+        float v[4][8];
 #pragma unroll
-        for (int c = threadIdx.x / 4; c < kTile; c += kBlock / 4) {
-            const int64_t row = chunk_c * kTile + c;            // of the transpose
-            if (row >= a.n_cols) break;
-            const float *from = tile + b * kMxBlock * kTile + (c + 16 * b) % kTile;
-            float v[4][8];
-            uint32_t most = 0;
+        for (int k = 0; k < kMxBlock; ++k) v[k / 8][k % 8] = from[k * kMxChunk];
+        uint32_t most = 0;
 #pragma unroll
-            for (int k = 0; k < kMxBlock; ++k) {
-                v[k / 8][k % 8] = from[k * kTile];
-                most = max(most, magnitude(v[k / 8][k % 8]));
-            }
-            const uint32_t byte = scale_byte<STOCHASTIC>(most);
-            uint32_t word[4];
+        for (int g = 0; g < 4; ++g) most = max(most, magnitude(largest<8>(v[g])));
+        const uint32_t byte = scale_byte<STOCHASTIC>(most);
+        uint32_t word[4];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                Rand128 rnd{};
-                if (STOCHASTIC) rnd = random_words(a.seed + 1, row, chunk_r * (kTile / 8) + b * 4 + g);
-                word[g] = codes_of<STOCHASTIC>(v[g], byte, rnd);
-            }
-            uint32_t scales = byte << (8 * b);
-            scales |= moved<kSwap1>(scales);
-            scales |= moved<kSwap2>(scales);
-            *reinterpret_cast<uint4 *>(a.codes_t + row * a.pitch_t + chunk_r * kMxChunkBytes + b * 16) = make_uint4(word[0], word[1], word[2], word[3]);
-            if (b == 0) *reinterpret_cast<uint32_t *>(a.scales_t + (chunk_r * a.n_cols + row) * 4) = scales;
-        }
+        for (int g = 0; g < 4; ++g)
+            word[g] = STOCHASTIC ? stochastic_codes(v[g], byte, random_words(a.seed + 1, row, tile_r * (kRows / 8) + b * 4 + g)) : nearest_codes(v[g], byte);
+        const uint32_t scales = byte << (8 * b) | moved<kSwap1>(byte << (8 * b));
+        const int64_t chunk_r = tile_r / 2, part = tile_r % 2;  // of the transpose's columns
+        *reinterpret_cast<uint4 *>(a.codes_t + row * a.pitch_t + chunk_r * kMxChunkBytes + (part * 2 + b) * 16) = make_uint4(word[0], word[1], word[2], word[3]);
+        if (b == 0) *reinterpret_cast<uint16_t *>(a.scales_t + (chunk_r * a.n_cols + row) * 4 + part * 2) = (uint16_t)scales;
     }
 }
 
 // 8 values of one word of codes.
 __device__ __forceinline__ void values_of(uint32_t word, uint32_t byte, float (&v)[8])
 {
-    const float scale = __builtin_bit_cast(float, byte == 0 ? 0x400000u : byte << 23);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t code = word >> (4 * j) & 7u, exponent = code >> 1, odd = code & 1u;
-        // 0, 1/2, then (1 + odd / 2) 2^(exponent - 1)
-        const uint32_t bits = exponent ? (126u + exponent) << 23 | odd << 22 : odd ? 126u << 23 : 0u;
-        const float m = __builtin_bit_cast(float, bits | (word >> (4 * j + 3) & 1u) << 31) * scale;
-        v[j] = byte == 255 ? __builtin_nanf("") : m;
-    }
+    // the conversion goes by the scale's exponent; 255 is NaN
+    const float scale = __builtin_bit_cast(float, byte << 23), nan = __builtin_nanf("");
+    const auto put = [&](int j, auto pair) {
+        v[j] = byte == 255 ? nan : pair[0];
+        v[j + 1] = byte == 255 ? nan : pair[1];
+    };
+    put(0, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 0));
+    put(2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 1));
+    put(4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 2));
+    put(6, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(word, scale, 3));
 }
 
 template <typename T, int VW, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void mx4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int64_t n_rows, int64_t n_cols, int64_t written,
                                                                 int64_t pitch, T *x, int64_t ld, int64_t granules)
 {
-    const int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-    const int64_t row = at / granules, g = at % granules;
+    const uint64_t at = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+    const int64_t row = at >> 32 ? at / (uint64_t)granules : (uint32_t)at / (uint32_t)granules, g = at - row * granules;
     if (row >= n_rows) return;
     float v[8];
     if (g * 8 < n_cols) values_of(*reinterpret_cast<const uint32_t *>(codes + row * pitch + g * 4), scales[(g / 16 * n_rows + row) * 4 + g / 4 % 4], v);
@@ -205,12 +264,11 @@ __global__ __launch_bounds__(kBlock) void mx4_dequantize_kernel(const uint8_t *c
 template <typename T, int VW>
 void launch_quantize(const MxArgs &a, int32_t rounding, int64_t blocks, hipStream_t st)
 {
-    const bool rows = a.codes, cols = a.codes_t;
     auto go = [&](auto stochastic) {
         constexpr bool S = decltype(stochastic)::value;
-        if (rows && cols) mx4_quantize_kernel<T, VW, true, true, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
-        else if (rows)    mx4_quantize_kernel<T, VW, true, false, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
-        else              mx4_quantize_kernel<T, VW, false, true, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
+        if (!a.codes_t)   mx4_quantize_rows_kernel<T, VW, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
+        else if (a.codes) mx4_quantize_kernel<T, VW, true, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
+        else              mx4_quantize_kernel<T, VW, false, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
     };
     if (rounding == ADAQP_MX4_STOCHASTIC) go(std::true_type());
     else                                  go(std::false_type());
@@ -233,14 +291,16 @@ hipError_t launch_dequantize(const uint8_t *codes, const uint8_t *scales, int64_
     const int64_t granules = (written + 7) / 8, blocks = (n_rows * granules + kBlock - 1) / kBlock;
     if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     constexpr int VW = 16 / sizeof(T);
-    const bool wide = whole || (aligned_to(x, 16) && ld % VW == 0);
+    int vw = VW;
+    while (vw > 1 && (!aligned_to(x, vw * sizeof(T)) || ld % vw != 0)) vw /= 2;
     auto go = [&](auto vw, auto lines) {
         mx4_dequantize_kernel<T, decltype(vw)::value, decltype(lines)::value>
             <<<(uint32_t)blocks, kBlock, 0, st>>>(codes, scales, n_rows, n_cols, written, mx_pitch(n_cols), (T *)x, ld, granules);
     };
-    if (whole)     go(std::integral_constant<int, VW>(), std::true_type());
-    else if (wide) go(std::integral_constant<int, VW>(), std::false_type());
-    else           go(std::integral_constant<int, 1>(), std::false_type());
+    if (whole)              go(std::integral_constant<int, VW>(), std::true_type());
+    else if (vw == VW)      go(std::integral_constant<int, VW>(), std::false_type());
+    else if (vw == VW / 2)  go(std::integral_constant<int, VW / 2>(), std::false_type());
+    else                    go(std::integral_constant<int, 1>(), std::false_type());
     return hipGetLastError();
 }
 
@@ -270,12 +330,14 @@ extern "C" int adaqp_mx4_quantize(const void *x_dev, int64_t ld, int64_t n_rows,
     if (n_rows == 0 || n_cols == 0 || (!codes_dev && !codes_t_dev)) return ADAQP_OK;
     if (!x_dev || ld < n_cols || !aligned_to(x_dev, element_bytes(type))) return ADAQP_EINVAL;
     if ((codes_dev && !valid_mx(codes_dev, scales_dev)) || (codes_t_dev && !valid_mx(codes_t_dev, scales_t_dev))) return ADAQP_EINVAL;
-    MxArgs a{x_dev, ld, n_rows, n_cols, mx_chunks(n_cols), seed, codes_dev, scales_dev, codes_t_dev, scales_t_dev, mx_pitch(n_cols), mx_pitch(n_rows)};
-    const int64_t blocks = a.tiles_c * mx_chunks(n_rows);
+    // the columns' form writes whole chunks of 128 rows: two tiles of 64
+    const int64_t tiles_r = mx_chunks(n_rows) * 2, tiles_c = mx_chunks(n_cols), row_blocks = (n_cols + kMxBlock - 1) / kMxBlock;
+    const int64_t blocks = ((codes_t_dev ? tiles_r * tiles_c : (n_rows * row_blocks + kBlock / 2 - 1) / (kBlock / 2)) + 7) / 8 * 8;
     if (blocks > 0x7FFFFFFF) return ADAQP_ESIZE;
-    // a vector may not be past the last column unless the row's lines are the matrix's own; load_granule takes the last columns one by one
-    int vw = (int)(16 / element_bytes(type));
-    while (vw > 1 && (!aligned_to(x_dev, vw * element_bytes(type)) || ld % vw != 0)) vw /= 2;
+    MxArgs a{x_dev, ld, n_rows, n_cols, (uint32_t)tiles_r, (uint32_t)tiles_c, (uint32_t)row_blocks, seed, codes_dev, scales_dev, codes_t_dev, scales_t_dev, mx_pitch(n_cols),
+             mx_pitch(n_rows)};
+    const int64_t bytes = element_bytes(type);
+    const int vw = whole_lines(x_dev, ld, bytes) ? (int)(16 / bytes) : vector_elements(x_dev, ld, n_cols, bytes);       // in its own lines a vector may pass the last column
     if (type == ADAQP_F32) ADAQP_HIP_TRY((launch_quantize<float>(a, vw, rounding, blocks, (hipStream_t)stream)));
     else                   ADAQP_HIP_TRY((launch_quantize<__bf16>(a, vw, rounding, blocks, (hipStream_t)stream)));
     return ADAQP_OK;

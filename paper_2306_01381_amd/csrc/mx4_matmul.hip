@@ -12,6 +12,7 @@ namespace adaqp {
 namespace {
 
 constexpr int kStepChunks = 2;                      // scale words
+constexpr int64_t kMostDepth = (int64_t)1 << 25;    // columns of the operands: a tile's places in them are 32-bit
 
 typedef int mx_codes __attribute__((ext_vector_type(8)));       // of which 4-bit codes fill the first half
 typedef float mx_sums __attribute__((ext_vector_type(16)));
@@ -23,48 +24,88 @@ struct MulArgs {
     int64_t written;                                // columns of out: n, or its whole lines
     int64_t pitch;                                  // of a row of codes, both operands
     int64_t chunks;                                 // scale words of a row
-    int64_t steps, steps_per_split;
+    int64_t steps, steps_per_split, splits;
     int64_t tiles_m, tiles_n;
 };
-
-// A step's scales of ROWS rows into the LDS, [2][ROWS] words.
-template <int ROWS>
-__device__ __forceinline__ void load_scales(const uint8_t *scales, int64_t row0, int64_t n_rows, int64_t chunks, int64_t step, uint8_t *lds)
-{
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-#pragma unroll
-    for (int i = 0; i < (ROWS * kStepChunks + kBlock - 1) / kBlock; ++i) {
-        const int first = (i * kWavesPerBlock + wave) * kWave;  // words
-        if (ROWS * kStepChunks < kBlock && first >= ROWS * kStepChunks) break;
-        const int64_t row = row0 + first % ROWS + lane, chunk = step * kStepChunks + first / ROWS;
-        load_to_lds_4(row < n_rows && chunk < chunks ? (const void *)(scales + (chunk * n_rows + row) * 4) : zeros(), lds + first * 4);
-    }
-}
 
 template <int BM, int BN>
 struct Stage {
     uint8_t a[BM * kLine], b[BN * kLine];
-    uint8_t sa[BM * kStepChunks * 4], sb[BN * kStepChunks * 4];
+    uint32_t scales[kStepChunks * (BM + BN)];       // [2][BM], then [2][BN]
 };
 
-template <typename T, int BM, int BN>
+// What lanes load whose scales do not exist: 2^-127, times the other operand's too, leaves nothing of whatever codes.
+__device__ const uint32_t smallest_scales = 0;
+
+// A workgroup's loads of a step, the same number in every wave.
+template <int BM, int BN>
+struct StepLoads {
+    static constexpr int kScaleLoads = kStepChunks * (BM + BN) / kBlock;
+    static constexpr int kLoads = TileLoads<BM>::kLoads + TileLoads<BN>::kLoads + kScaleLoads;
+    TileLoads<BM> a;
+    TileLoads<BN> b;
+    const uint8_t *from_a, *from_b;
+    const uint8_t *from_scale[kScaleLoads];
+    int64_t scale_stride[kScaleLoads];              // from step to step
+    int scale_chunk[kScaleLoads];
+    uint32_t scale[kScaleLoads], to_scale;
+    uint64_t missing;
+    int chunks;
+
+    // Of the words [2][BM], [2][BN] a wave's load takes 64.
+    __device__ __forceinline__ StepLoads(const MulArgs &g, int64_t row0, int64_t col0) : a(row0, g.m, g.pitch), b(col0, g.n, g.pitch)
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        from_a = g.a_codes + row0 * g.pitch;
+        from_b = g.b_codes + col0 * g.pitch;
+        chunks = (int)g.chunks;
+        missing = (uint64_t)&smallest_scales;
+        to_scale = wave * kWave * 4;
+#pragma unroll
+        for (int i = 0; i < kScaleLoads; ++i) {
+            int at = (i * kWavesPerBlock + wave) * kWave;
+            const bool of_b = at >= kStepChunks * BM;
+            at -= of_b ? kStepChunks * BM : 0;
+            const int rows = of_b ? BN : BM;
+            const int64_t n = of_b ? g.n : g.m, first = of_b ? col0 : row0;
+            scale_chunk[i] = at / rows;
+            scale_stride[i] = n * 4 * kStepChunks;
+            from_scale[i] = (of_b ? g.b_scales : g.a_scales) + (scale_chunk[i] * n + first) * 4;
+            scale[i] = min((uint32_t)(at % rows + threadIdx.x % kWave), (uint32_t)min((int64_t)rows, n - first) - 1) * 4;
+        }
+    }
+
+    // Load i of a step.  The last step of an odd number of chunks has half a line, and the smallest scales for the other.
+    __device__ __forceinline__ void load(int i, int step, const Stage<BM, BN> &s) const
+    {
+        constexpr int kA = TileLoads<BM>::kLoads, kB = TileLoads<BN>::kLoads;
+        const bool half = (step + 1) * kStepChunks > chunks;
+        if (i < kA)           a.template load<true>(i, from_a + (int64_t)step * kLine, TileLoads<BM>::place(s.a), half);
+        else if (i < kA + kB) b.template load<true>(i - kA, from_b + (int64_t)step * kLine, TileLoads<BN>::place(s.b), half);
+        else {
+            i -= kA + kB;
+            const bool there = step * kStepChunks + scale_chunk[i] < chunks;
+            const uint64_t from = (uint64_t)from_scale[i] + step * scale_stride[i], mask = there ? ~(uint64_t)0 : 0;
+            load_to_lds_4((const void *)((from & mask) | (missing & ~mask)), scale[i] & (uint32_t)mask,
+                          __builtin_amdgcn_readfirstlane(lds_offset(s.scales) + to_scale + i * kBlock * 4));
+        }
+    }
+};
+
+template <typename T, int BM, int BN, int STAGES>
 __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
 {
     constexpr int FM = BM / 64, FN = BN / 64;       // 32 x 32 parts of a wave
-    __shared__ Stage<BM, BN> stage[2];
-    const int64_t tiles = g.tiles_m * g.tiles_n;
-    const int64_t split = blockIdx.x / tiles, tile = blockIdx.x % tiles;
-    const int64_t row0 = tile / g.tiles_n * BM, col0 = tile % g.tiles_n * BN;
+    __shared__ Stage<BM, BN> stage[STAGES];
+    using Loads = StepLoads<BM, BN>;
+    const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
+    if (place.part < 0) return;
+    const int64_t split = place.part, row0 = place.row * BM, col0 = place.col * BN;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
     const int wm = wave / 2 * (BM / 2), wn = wave % 2 * (BN / 2);
-    const int64_t begin = split * g.steps_per_split, end = min(begin + g.steps_per_split, g.steps);
+    const int begin = (int)(split * g.steps_per_split), steps = (int)min(g.steps_per_split, g.steps - begin);
+    const Loads loads(g, row0, col0);
 
-    auto load = [&](int64_t step, Stage<BM, BN> &s) {
-        load_lines<BM>(g.a_codes, row0, g.m, g.pitch, step, s.a);
-        load_lines<BN>(g.b_codes, col0, g.n, g.pitch, step, s.b);
-        load_scales<BM>(g.a_scales, row0, g.m, g.chunks, step, s.sa);
-        load_scales<BN>(g.b_scales, col0, g.n, g.chunks, step, s.sb);
-    };
     mx_sums sums[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -73,51 +114,92 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
 #pragma unroll
             for (int q = 0; q < 16; ++q) sums[i][j][q] = 0.0f;
 
-    if (begin < end) load(begin, stage[0]);
-    landed();
-    for (int64_t step = begin; step < end; ++step) {
-        const Stage<BM, BN> &s = stage[(step - begin) % 2];
-        if (step + 1 < end) load(step + 1, stage[(step - begin + 1) % 2]);
+    // The operands of a quarter of a step, 64 columns: read from the LDS while the quarter before is multiplied.
+    struct Quarter { int4 a[FM], b[FN]; } quarter[2];
+    uint32_t sa[kStepChunks][FM], sb[kStepChunks][FN];      // scales of this lane's rows; the upper half of a wave has the odd blocks
+    auto read = [&](const Stage<BM, BN> &s, int at, Quarter &to) {
 #pragma unroll
-        for (int c = 0; c < kStepChunks; ++c) {
-            uint32_t sa[FM], sb[FN];                // of this lane's rows; the upper half of a wave has the odd blocks
+        for (int i = 0; i < FM; ++i) to.a[i] = *reinterpret_cast<const int4 *>(line_part(s.a, wm + i * 32 + r, at * 2 + h));
 #pragma unroll
-            for (int i = 0; i < FM; ++i) sa[i] = *reinterpret_cast<const uint32_t *>(s.sa + (c * BM + wm + i * 32 + r) * 4) >> (8 * h);
+        for (int j = 0; j < FN; ++j) to.b[j] = *reinterpret_cast<const int4 *>(line_part(s.b, wn + j * 32 + r, at * 2 + h));
+    };
+    auto read_scales = [&](const Stage<BM, BN> &s, int c) {
 #pragma unroll
-            for (int j = 0; j < FN; ++j) sb[j] = *reinterpret_cast<const uint32_t *>(s.sb + (c * BN + wn + j * 32 + r) * 4) >> (8 * h);
+        for (int i = 0; i < FM; ++i) sa[c][i] = s.scales[c * BM + wm + i * 32 + r] >> (8 * h);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const int part = c * 4 + q * 2 + h;
-                mx_codes a[FM], b[FN];
-                auto codes = [&](const uint8_t *lines, int row) {
-                    const int4 v = *reinterpret_cast<const int4 *>(line_part(lines, row, part));
-                    return mx_codes{v.x, v.y, v.z, v.w, 0, 0, 0, 0};
-                };
+        for (int j = 0; j < FN; ++j) sb[c][j] = s.scales[kStepChunks * BM + c * BN + wn + j * 32 + r] >> (8 * h);
+    };
+    // `between(p)` is done behind product p of the quarter's FM * FN.
+    auto multiply = [&](const Quarter &f, int at, auto between) {
+        const int c = at / 2;
 #pragma unroll
-                for (int i = 0; i < FM; ++i) a[i] = codes(s.a, wm + i * 32 + r);
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-                for (int j = 0; j < FN; ++j) b[j] = codes(s.b, wn + j * 32 + r);
-#pragma unroll
-                for (int i = 0; i < FM; ++i)
-#pragma unroll
-                    for (int j = 0; j < FN; ++j)
-                        sums[i][j] = q == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[i], b[j], sums[i][j], 4, 4, 0, (int)sa[i], 0, (int)sb[j])
-                                            : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a[i], b[j], sums[i][j], 4, 4, 2, (int)sa[i], 2, (int)sb[j]);
+            for (int j = 0; j < FN; ++j) {
+                const mx_codes a{f.a[i].x, f.a[i].y, f.a[i].z, f.a[i].w, 0, 0, 0, 0}, b{f.b[j].x, f.b[j].y, f.b[j].z, f.b[j].w, 0, 0, 0, 0};
+                sums[i][j] = at % 2 == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sums[i][j], 4, 4, 0, (int)sa[c][i], 0, (int)sb[c][j])
+                                         : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sums[i][j], 4, 4, 2, (int)sa[c][i], 2, (int)sb[c][j]);
+                between(i * FN + j);
             }
-        }
-        landed();
-    }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto nothing = [](int) {};
 
-    T *out = (T *)g.out + (split ? split * g.m * g.n : 0);
+    // Up to STAGES steps are under way.  A step's last quarter is multiplied behind the barrier after which the next step is in the LDS and its own buffer
+    // free, and the loads into that buffer are issued between its products.  No branches: across one the compiler would take products to the other side
+    // of the barrier.
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+        if (s < steps)
+#pragma unroll
+            for (int l = 0; l < Loads::kLoads; ++l) loads.load(l, begin + s, stage[s]);
+    if (steps >= STAGES) arrived<Loads::kLoads * (STAGES - 1)>();
+    else                 arrived<0>();
+    read_scales(stage[0], 0);
+    read(stage[0], 0, quarter[0]);
+    int now = 0;
+    auto one = [&](int step, auto more) {
+        constexpr bool kMore = decltype(more)::value;
+        const Stage<BM, BN> &s = stage[now];
+        now = now + 1 == STAGES ? 0 : now + 1;
+        read_scales(s, 1);
+#pragma unroll
+        for (int at = 0; at < 3; ++at) {
+            read(s, at + 1, quarter[(at + 1) % 2]);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(quarter[at % 2], at, nothing);
+        }
+        arrived<kMore ? Loads::kLoads * (STAGES - 2) : 0>();
+        read_scales(stage[now], 0);
+        read(stage[now], 0, quarter[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(quarter[1], 3, [&](int p) {
+            if constexpr (kMore) {
+#pragma unroll
+                for (int l = p * Loads::kLoads / (FM * FN); l < (p + 1) * Loads::kLoads / (FM * FN); ++l) loads.load(l, step + STAGES, s);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+    };
+    int i = 0;
+    for (; i + STAGES < steps; ++i) one(begin + i, std::true_type());
+    for (; i < steps; ++i) one(begin + i, std::false_type());
+
+    // lane's part of a place, and the wave's
+    T *out = (T *)g.out + (split * g.m + row0 + wm) * g.ldo + col0 + wn;
+    const int64_t mine = (int64_t)(h * 4) * g.ldo + r;
+    const int rows = (int)min(g.m - row0 - wm, (int64_t)BM), cols = (int)min(g.n - col0 - wn, (int64_t)BN), written = (int)min(g.written - col0 - wn, (int64_t)BN);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
+        for (int q = 0; q < 16; ++q) {
+            const int row = i * 32 + q / 4 * 8 + q % 4;
+            if (row + h * 4 >= rows) continue;
+            T *to = out + row * g.ldo + mine;
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                const int64_t row = row0 + wm + i * 32 + q / 4 * 8 + h * 4 + q % 4, col = col0 + wn + j * 32 + r;
-                if (row < g.m && col < g.written) out[row * g.ldo + col] = col < g.n ? (T)sums[i][j][q] : (T)0.0f;
-            }
+            for (int j = 0; j < FN; ++j)
+                if (j * 32 + r < written) to[j * 32] = j * 32 + r < cols ? (T)sums[i][j][q] : (T)0.0f;
+        }
 }
 
 // The splits' sums, in order; columns from n to `written` are zeros.
@@ -147,7 +229,7 @@ MulShape mul_shape(int64_t m, int64_t n, int64_t k)
         s.tiles_n = (n + t - 1) / t;
         return s.tiles_m * s.tiles_n;
     };
-    if (tiles(128) < 256) tiles(64);
+    if (tiles(256) < 256 && tiles(128) < 256) tiles(64);
     const int64_t blocks = s.tiles_m * s.tiles_n;
     s.steps = (mx_chunks(k) + kStepChunks - 1) / kStepChunks;
     int64_t splits = blocks >= 256 || blocks == 0 ? 1 : 512 / blocks;
@@ -162,15 +244,16 @@ MulShape mul_shape(int64_t m, int64_t n, int64_t k)
 template <typename T>
 void launch_tiles(const MulArgs &g, const MulShape &s, hipStream_t st)
 {
-    const uint32_t blocks = (uint32_t)(s.tiles_m * s.tiles_n * s.splits);
-    if (s.tile == 128) mx4_matmul_kernel<T, 128, 128><<<blocks, kBlock, 0, st>>>(g);
-    else               mx4_matmul_kernel<T, 64, 64><<<blocks, kBlock, 0, st>>>(g);
+    const uint32_t blocks = (uint32_t)tile_blocks(s.tiles_m * s.tiles_n, s.splits);
+    if (s.tile == 256) mx4_matmul_kernel<T, 256, 256, 2><<<blocks, kBlock, 0, st>>>(g);
+    else if (s.tile == 128) mx4_matmul_kernel<T, 128, 128, 2><<<blocks, kBlock, 0, st>>>(g);
+    else               mx4_matmul_kernel<T, 64, 64, 4><<<blocks, kBlock, 0, st>>>(g);
 }
 
 int check_sizes(int64_t m, int64_t n, int64_t k)
 {
     if (m < 0 || n < 0 || k < 0) return ADAQP_EINVAL;
-    return m >= kMxMost || n >= kMxMost || k >= kMxMost || (m + 63) / 64 * ((n + 63) / 64) >= 0x7FFFFFFF ? ADAQP_ESIZE : ADAQP_OK;
+    return m >= kMxMost || n >= kMxMost || k > kMostDepth || (m + 63) / 64 * ((n + 63) / 64) >= 0x3FFFFFFF ? ADAQP_ESIZE : ADAQP_OK;
 }
 
 }  // namespace
@@ -201,7 +284,7 @@ extern "C" int adaqp_mx4_matmul(const uint8_t *a_codes_dev, const uint8_t *a_sca
         if (workspace_bytes < s.bytes) return ADAQP_ESIZE;
     }
     MulArgs g{a_codes_dev, a_scales_dev, b_codes_dev, b_scales_dev, out_dev, m, n, ldo, 0, mx_pitch(k), mx_chunks(k), s.steps, s.steps_per_split,
-              s.tiles_m, s.tiles_n};
+              s.splits, s.tiles_m, s.tiles_n};
     const hipStream_t st = (hipStream_t)stream;
     const int64_t line = 128 / element_bytes(type);
     const int64_t written = whole_lines(out_dev, ldo, element_bytes(type)) ? (n + line - 1) / line * line : n;

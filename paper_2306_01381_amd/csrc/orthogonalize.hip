@@ -43,15 +43,19 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// Sums of squares of a share of each matrix: blocks [x] of matrix [y].
+// Sums of squares of a share of each matrix: blocks [x] of matrix [y], runs of kBlock columns of a row.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void update_norm_kernel(const T *g, int64_t ldg, int64_t stride, int64_t n_rows, int64_t n_cols, double *partial)
 {
     __shared__ double lds[kWavesPerBlock];
     g += blockIdx.y * stride;
+    const uint32_t runs = (uint32_t)((n_cols + kBlock - 1) / kBlock);
+    const int64_t total = n_rows * runs;
     double sum = 0.0;
-    for (int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x; at < n_rows * n_cols; at += (int64_t)gridDim.x * kBlock) {
-        const double v = (double)(float)g[at / n_cols * ldg + at % n_cols];
+#pragma unroll 4
+    for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
+        const uint32_t row = (uint32_t)((uint64_t)at / runs), col = ((uint32_t)at - row * runs) * kBlock + threadIdx.x;
+        const double v = col < n_cols ? (double)(float)g[row * ldg + col] : 0.0;
         sum = fma(v, v, sum);
     }
     sum = block_sum(sum, lds);
@@ -69,16 +73,25 @@ __global__ __launch_bounds__(kBlock) void update_split_kernel(const T *g, int64_
     g += blockIdx.z * stride;
     same += blockIdx.z * held_bytes;
     other += blockIdx.z * held_bytes;
+    constexpr int kEach = kPad * kPad / kBlock;
+    const int64_t row0 = (int64_t)blockIdx.y * kPad, col0 = (int64_t)blockIdx.x * kPad;
+    const int c = threadIdx.x % kPad, r0 = threadIdx.x / kPad;
+    float v[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int64_t row = row0 + r0 + i * (kBlock / kPad), col = col0 + c;
+        v[i] = row < n_rows && col < n_cols ? (float)g[row * ldg + col] : 0.0f;
+    }
     const double total = block_sum((int)threadIdx.x < n_partial ? partial[blockIdx.z * n_partial + threadIdx.x] : 0.0, lds);
     const double scale = ldexp(1.0 / (sqrt(total) + eps), power);
-    const int64_t row0 = (int64_t)blockIdx.y * kPad, col0 = (int64_t)blockIdx.x * kPad;
-    const int c = threadIdx.x % kPad;
-    for (int r = threadIdx.x / kPad; r < kPad; r += kBlock / kPad) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int r = r0 + i * (kBlock / kPad);
         const int64_t row = row0 + r, col = col0 + c;
-        const float v = row < n_rows && col < n_cols ? (float)((double)(float)g[row * ldg + col] * scale) : 0.0f;
-        tile[r][c] = v;
+        v[i] = row < n_rows && col < n_cols ? (float)((double)v[i] * scale) : 0.0f;       // behind the edge also where the scale is not finite
+        tile[r][c] = v[i];
         _Float16 hi, lo;
-        split(v, hi, lo);
+        split(v[i], hi, lo);
         uint8_t *to = same + held_at(row, col, pitch_same);
         *reinterpret_cast<_Float16 *>(to) = hi;
         *reinterpret_cast<_Float16 *>(to + 64) = lo;
@@ -98,7 +111,8 @@ enum Product { GRAM, POLY, STEP, LAST };
 struct ProductArgs {
     const uint8_t *p, *q;                           // D = p q^T
     int64_t rows, cols;                             // of D, padded
-    int64_t lines;                                  // of a row of p and q
+    int64_t lines;                                  // of a row of p and q that hold columns
+    int64_t pitch;                                  // of p and q
     uint8_t *same, *other;                          // D and its transpose, held
     int64_t pitch_same, pitch_other;
     int64_t bytes_p, bytes_q, bytes_d;              // from matrix to matrix
@@ -109,12 +123,12 @@ struct ProductArgs {
     int64_t tiles_r, tiles_c;
 };
 
-template <Product KIND, typename T, int TILE>
+template <Product KIND, typename T, int TILE, int STAGES>
 __global__ __launch_bounds__(kBlock) void update_product_kernel(ProductArgs g)
 {
     constexpr bool kSymmetric = KIND == GRAM || KIND == POLY;
     constexpr int F = TILE / 64;                    // 32 x 32 parts of a wave, both ways
-    __shared__ struct { uint8_t p[TILE * kLine], q[TILE * kLine]; } stage[2];
+    __shared__ struct { uint8_t p[TILE * kLine], q[TILE * kLine]; } stage[STAGES];
     int64_t tr, tc;
     if (kSymmetric) {                               // tiles below and on the diagonal, row by row
         tr = (int64_t)((sqrtf(8.0f * blockIdx.x + 1.0f) - 1.0f) * 0.5f);
@@ -122,11 +136,13 @@ __global__ __launch_bounds__(kBlock) void update_product_kernel(ProductArgs g)
         while ((tr + 1) * (tr + 2) / 2 <= blockIdx.x) ++tr;
         tc = blockIdx.x - tr * (tr + 1) / 2;
     } else {
-        tr = blockIdx.x / g.tiles_c;
-        tc = blockIdx.x % g.tiles_c;
+        const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_r, (uint32_t)g.tiles_c, 1);
+        if (place.part < 0) return;
+        tr = place.row;
+        tc = place.col;
     }
     const uint8_t *p = g.p + blockIdx.y * g.bytes_p, *q = g.q + blockIdx.y * g.bytes_q;
-    const int64_t row0 = tr * TILE, col0 = tc * TILE, pitch = g.lines * kLine;
+    const int64_t row0 = tr * TILE, col0 = tc * TILE, pitch = g.pitch;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
 
@@ -138,36 +154,74 @@ __global__ __launch_bounds__(kBlock) void update_product_kernel(ProductArgs g)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sums[i][j][e] = 0.0f;
 
-    auto load = [&](int64_t line, auto &s) {
-        load_lines<TILE>(p, row0, g.rows, pitch, line, s.p);
-        load_lines<TILE>(q, col0, g.cols, pitch, line, s.q);
+    const TileLoads<TILE> of_p(row0, g.rows, pitch), of_q(col0, g.cols, pitch);
+    constexpr int kLoads = 2 * TileLoads<TILE>::kLoads;
+    const uint8_t *from_p = p + row0 * pitch, *from_q = q + col0 * pitch;
+    // Load i of a line of both operands.
+    auto load = [&](int i, int line, const auto &s) {
+        if (i < kLoads / 2) of_p.template load<false>(i, from_p + (int64_t)line * kLine, TileLoads<TILE>::place(s.p));
+        else                of_q.template load<false>(i - kLoads / 2, from_q + (int64_t)line * kLine, TileLoads<TILE>::place(s.q));
     };
-    load(0, stage[0]);
-    landed();
-    for (int64_t line = 0; line < g.lines; ++line) {
-        auto &s = stage[line % 2];
-        if (line + 1 < g.lines) load(line + 1, stage[(line + 1) % 2]);
+    // The operands of half a line, 16 columns: read from the LDS while the half before is multiplied.
+    struct Half { half8 ph[F], pl[F], qh[F], ql[F]; } half[2];
+    auto read = [&](const auto &s, int k, Half &to) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {               // 16 columns each
-            half8 ph[F], pl[F], qh[F], ql[F];
+        for (int i = 0; i < F; ++i) {
+            to.ph[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, k * 2 + h));
+            to.pl[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, 4 + k * 2 + h));
+            to.qh[i] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + i * 32 + r, k * 2 + h));
+            to.ql[i] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + i * 32 + r, 4 + k * 2 + h));
+        }
+    };
+    // `between(p)` is done behind product p of the half's 3 F F.
+    auto multiply = [&](const Half &f, auto between) {
 #pragma unroll
-            for (int i = 0; i < F; ++i) {
-                ph[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, k * 2 + h));
-                pl[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, 4 + k * 2 + h));
-                qh[i] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + i * 32 + r, k * 2 + h));
-                ql[i] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + i * 32 + r, 4 + k * 2 + h));
-            }
+        for (int w = 0; w < 3; ++w)                 // the small ones first
 #pragma unroll
             for (int i = 0; i < F; ++i)
 #pragma unroll
                 for (int j = 0; j < F; ++j) {
-                    sums[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[i], qh[j], sums[i][j], 0, 0, 0);
-                    sums[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], ql[j], sums[i][j], 0, 0, 0);
-                    sums[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[i], qh[j], sums[i][j], 0, 0, 0);
+                    sums[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.pl[i] : f.ph[i], w == 1 ? f.ql[j] : f.qh[j], sums[i][j], 0, 0, 0);
+                    between((w * F + i) * F + j);
                 }
-        }
-        landed();
-    }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto nothing = [](int) {};
+
+    // Up to STAGES lines are under way.  A line's second half is multiplied behind the barrier after which the next line is in the LDS and its own buffer
+    // free, and the loads into that buffer are issued between its products.  No branches: across one the compiler would take products to the other side
+    // of the barrier.
+    const int lines = (int)g.lines;
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+        if (s < lines)
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l) load(l, s, stage[s]);
+    if (lines >= STAGES) arrived<kLoads * (STAGES - 1)>();
+    else                 arrived<0>();
+    read(stage[0], 0, half[0]);
+    int now = 0;
+    auto one = [&](int line, auto more) {
+        constexpr bool kMore = decltype(more)::value;
+        const auto &s = stage[now];
+        now = now + 1 == STAGES ? 0 : now + 1;
+        read(s, 1, half[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(half[0], nothing);
+        arrived<kMore ? kLoads * (STAGES - 2) : 0>();
+        read(stage[now], 0, half[0]);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(half[1], [&](int p) {
+            if constexpr (kMore) {
+#pragma unroll
+                for (int l = p * kLoads / (3 * F * F); l < (p + 1) * kLoads / (3 * F * F); ++l) load(l, line + STAGES, s);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+    };
+    int line = 0;
+    for (; line + STAGES < lines; ++line) one(line, std::true_type());
+    for (; line < lines; ++line) one(line, std::false_type());
 
     uint8_t *same = g.same + blockIdx.y * g.bytes_d, *other = g.other + blockIdx.y * g.bytes_d;
 #pragma unroll
@@ -233,6 +287,9 @@ __global__ __launch_bounds__(kBlock) void update_scale_kernel(const T *g, int64_
 
 int64_t padded(int64_t v) { return (v + kPad - 1) / kPad * kPad; }
 
+// Bytes from row to row of a held matrix: an odd number of lines, so that the same line of all rows is spread over the L2's channels.
+int64_t held_pitch(int64_t cols) { return (cols / 32 | 1) * kLine; }
+
 struct UpdateLayout {
     bool flip;                                      // more rows than columns: X is the transpose
     int64_t n, m;                                   // padded, n of the smaller
@@ -247,9 +304,10 @@ UpdateLayout update_layout(int32_t n_matrices, int64_t n_rows, int64_t n_cols)
     u.flip = n_rows > n_cols;
     u.n = padded(u.flip ? n_cols : n_rows);
     u.m = padded(u.flip ? n_rows : n_cols);
-    u.big = u.n * u.m * 4;
-    u.small = u.n * u.n * 4;
-    u.norm_blocks = (n_rows * n_cols + 4 * kBlock - 1) / (4 * kBlock);
+    const int64_t of_x = u.n * held_pitch(u.m), of_xt = u.m * held_pitch(u.n);
+    u.big = of_x > of_xt ? of_x : of_xt;
+    u.small = u.n * held_pitch(u.n);
+    u.norm_blocks = (n_rows * ((n_cols + kBlock - 1) / kBlock) + 3) / 4;
     if (u.norm_blocks > kNormBlocks) u.norm_blocks = kNormBlocks;
     u.partial_at = 0;
     u.x_at = (n_matrices * u.norm_blocks * 8 + 255) / 256 * 256;
@@ -301,10 +359,10 @@ hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
     };
     const int64_t large = tiles(128);
     if (large * n_matrices >= 256) {
-        update_product_kernel<KIND, T, 128><<<dim3((uint32_t)large, (uint32_t)n_matrices), kBlock, 0, st>>>(g);
+        update_product_kernel<KIND, T, 128, 2><<<dim3((uint32_t)(kSymmetric ? large : tile_blocks(large, 1)), (uint32_t)n_matrices), kBlock, 0, st>>>(g);
     } else {
         const int64_t small = tiles(64);
-        update_product_kernel<KIND, T, 64><<<dim3((uint32_t)small, (uint32_t)n_matrices), kBlock, 0, st>>>(g);
+        update_product_kernel<KIND, T, 64, 4><<<dim3((uint32_t)(kSymmetric ? small : tile_blocks(small, 1)), (uint32_t)n_matrices), kBlock, 0, st>>>(g);
     }
     return hipGetLastError();
 }
@@ -325,7 +383,7 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
             g, ldg, stride_g, n_rows, n_cols, partial, (int)u.norm_blocks, eps, out, ldo, stride_o, written);
         return hipGetLastError();
     }
-    const int64_t lines_n = u.n / 32, lines_m = u.m / 32;
+    const int64_t lines_n = u.n / 32, lines_m = u.m / 32, pitch_n = held_pitch(u.n), pitch_m = held_pitch(u.m);
     uint8_t *x[2], *xt[2], *a = work + u.a_at, *q = work + u.q_at;
     for (int i = 0; i < 2; ++i) {
         x[i] = work + u.x_at + 2 * i * n_matrices * u.big;
@@ -333,7 +391,7 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
     }
     update_split_kernel<T><<<dim3((uint32_t)(padded(n_cols) / kPad), (uint32_t)(padded(n_rows) / kPad), (uint32_t)n_matrices), kBlock, 0, st>>>(
         g, ldg, stride_g, n_rows, n_cols, partial, (int)u.norm_blocks, eps, x_power[0], u.flip ? xt[0] : x[0], u.flip ? x[0] : xt[0],
-        (u.flip ? lines_n : lines_m) * kLine, (u.flip ? lines_m : lines_n) * kLine, u.big);
+        u.flip ? pitch_n : pitch_m, u.flip ? pitch_m : pitch_n, u.big);
     if (hipError_t e = hipGetLastError()) return e;
     for (int32_t s = 0; s < n_steps; ++s) {
         const int now = s % 2;
@@ -342,8 +400,9 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
         gram.p = gram.q = x[now];
         gram.rows = gram.cols = u.n;
         gram.lines = lines_m;
+        gram.pitch = pitch_m;
         gram.same = gram.other = a;
-        gram.pitch_same = gram.pitch_other = lines_n * kLine;
+        gram.pitch_same = gram.pitch_other = pitch_n;
         gram.bytes_p = gram.bytes_q = u.big;
         gram.bytes_d = u.small;
         gram.scale = ldexpf(1.0f, a_power[s] - 2 * x_power[s]);
@@ -351,6 +410,7 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
         ProductArgs poly = gram;
         poly.p = poly.q = a;
         poly.lines = lines_n;
+        poly.pitch = pitch_n;
         poly.same = poly.other = q;
         poly.bytes_p = poly.bytes_q = u.small;
         poly.scale = ldexpf(abc[2], q_power[s] - 2 * a_power[s]);
@@ -359,6 +419,7 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
         if (hipError_t e = launch_product<POLY, float>(poly, n_matrices, st)) return e;
         ProductArgs step{};
         step.lines = lines_n;
+        step.pitch = pitch_n;
         if (s + 1 < n_steps) {                      // X^T Q, stored both ways
             step.p = xt[now];
             step.q = q;
@@ -366,8 +427,8 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
             step.cols = u.n;
             step.same = xt[1 - now];
             step.other = x[1 - now];
-            step.pitch_same = lines_n * kLine;
-            step.pitch_other = lines_m * kLine;
+            step.pitch_same = pitch_n;
+            step.pitch_other = pitch_m;
             step.bytes_p = step.bytes_d = u.big;
             step.bytes_q = u.small;
             step.scale = ldexpf(1.0f, x_power[s + 1] - x_power[s] - q_power[s]);
