@@ -4,7 +4,8 @@
 // takes a tile of BM x BN outputs, a quarter each wave, and walks k in steps of 256 columns, a line of 128 bytes of a row.  The next step's codes and
 // scales go from memory straight into the LDS while the current one is multiplied.
 //
-// Where the tiles are few, k is split over workgroups; the parts' sums, fp32, are added in order by a second kernel.
+// Where the tiles are few, k is split over workgroups; the parts' sums, fp32, are added in order by a second kernel.  With at most 32 rows nothing is used
+// twice but those: a workgroup takes 32 columns of out, its eight waves share the lines of k and read them into registers, as many at a time as they can.
 #include "lines.hpp"
 #include "mx4.hpp"
 
@@ -40,7 +41,7 @@ __device__ const uint32_t smallest_scales = 0;
 // A workgroup's loads of a step, the same number in every wave.
 template <int BM, int BN>
 struct StepLoads {
-    static constexpr int kScaleLoads = kStepChunks * (BM + BN) / kBlock;
+    static constexpr int kScaleWords = kStepChunks * (BM + BN), kScaleLoads = (kScaleWords + kBlock - 1) / kBlock;
     static constexpr int kLoads = TileLoads<BM>::kLoads + TileLoads<BN>::kLoads + kScaleLoads;
     TileLoads<BM> a;
     TileLoads<BN> b;
@@ -48,11 +49,11 @@ struct StepLoads {
     const uint8_t *from_scale[kScaleLoads];
     int64_t scale_stride[kScaleLoads];              // from step to step
     int scale_chunk[kScaleLoads];
-    uint32_t scale[kScaleLoads], to_scale;
+    uint32_t scale[kScaleLoads], to_scale[kScaleLoads];
     uint64_t missing;
     int chunks;
 
-    // Of the words [2][BM], [2][BN] a wave's load takes 64.
+    // Of the words [2][BM], [2][BN] a wave's load takes 64; where they do not come out even, some are loaded twice.
     __device__ __forceinline__ StepLoads(const MulArgs &g, int64_t row0, int64_t col0) : a(row0, g.m, g.pitch), b(col0, g.n, g.pitch)
     {
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -60,10 +61,10 @@ struct StepLoads {
         from_b = g.b_codes + col0 * g.pitch;
         chunks = (int)g.chunks;
         missing = (uint64_t)&smallest_scales;
-        to_scale = wave * kWave * 4;
 #pragma unroll
         for (int i = 0; i < kScaleLoads; ++i) {
-            int at = (i * kWavesPerBlock + wave) * kWave;
+            int at = (i * kWavesPerBlock + wave) * kWave % kScaleWords;
+            to_scale[i] = at * 4;
             const bool of_b = at >= kStepChunks * BM;
             at -= of_b ? kStepChunks * BM : 0;
             const int rows = of_b ? BN : BM;
@@ -87,7 +88,7 @@ struct StepLoads {
             const bool there = step * kStepChunks + scale_chunk[i] < chunks;
             const uint64_t from = (uint64_t)from_scale[i] + step * scale_stride[i], mask = there ? ~(uint64_t)0 : 0;
             load_to_lds_4((const void *)((from & mask) | (missing & ~mask)), scale[i] & (uint32_t)mask,
-                          __builtin_amdgcn_readfirstlane(lds_offset(s.scales) + to_scale + i * kBlock * 4));
+                          lds_offset(s.scales) + to_scale[i]);
         }
     }
 };
@@ -202,42 +203,131 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
         }
 }
 
-// The splits' sums, in order; columns from n to `written` are zeros.
+constexpr int kFewRows = 32, kFewWaves = 8;
+
+// At most 32 rows: 32 columns of out, wave w takes the lines w, w + 8, ... of its part of k.
 template <typename T>
-__global__ __launch_bounds__(kBlock) void mx4_join_kernel(const float *parts, int64_t n_parts, int64_t m, int64_t n, int64_t written, T *out, int64_t ldo)
+__global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_rows_kernel(MulArgs g)
 {
-    for (int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x; at < m * written; at += (int64_t)gridDim.x * kBlock) {
-        const int64_t row = at / written, col = at % written;
+    constexpr int kLines = 2;                       // under way
+    __shared__ float parts[kFewWaves][kFewRows * 32];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+    const int64_t col0 = (int64_t)blockIdx.x * 32;
+    const int64_t row_a = min((int64_t)r, g.m - 1), row_b = min(col0 + r, g.n - 1);
+    const int64_t begin = blockIdx.y * g.steps_per_split, end = min(begin + g.steps_per_split, g.steps);
+    mx_sums sums;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) sums[q] = 0.0f;
+    for (int64_t step = begin + wave; step < end; step += kFewWaves * kLines) {
+        int4 a[kLines][4], b[kLines][4];
+        uint32_t sa[kLines][kStepChunks], sb[kLines][kStepChunks];
+#pragma unroll
+        for (int i = 0; i < kLines; ++i) {
+            const int64_t line = min(step + i * kFewWaves, end - 1);
+            const bool missing = step + i * kFewWaves >= end;
+            const int64_t half = (line + 1) * kStepChunks > g.chunks ? kLine / 2 : 0;  // the line ends there: its first half in the second's place
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int64_t at = line * kLine + (q * 2 + h) * 16 - (q >= 2 ? half : 0);
+                a[i][q] = *reinterpret_cast<const int4 *>(g.a_codes + row_a * g.pitch + at);
+                b[i][q] = *reinterpret_cast<const int4 *>(g.b_codes + row_b * g.pitch + at);
+            }
+#pragma unroll
+            for (int c = 0; c < kStepChunks; ++c) {
+                const int64_t chunk = min(line * kStepChunks + c, g.chunks - 1);
+                const bool none = missing || line * kStepChunks + c >= g.chunks;
+                const uint32_t wa = *reinterpret_cast<const uint32_t *>(g.a_scales + (chunk * g.m + row_a) * 4);
+                const uint32_t wb = *reinterpret_cast<const uint32_t *>(g.b_scales + (chunk * g.n + row_b) * 4);
+                sa[i][c] = none ? 0 : wa >> (8 * h);            // the smallest scales: nothing is left of the product
+                sb[i][c] = none ? 0 : wb >> (8 * h);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kLines; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const mx_codes x{a[i][q].x, a[i][q].y, a[i][q].z, a[i][q].w, 0, 0, 0, 0}, y{b[i][q].x, b[i][q].y, b[i][q].z, b[i][q].w, 0, 0, 0, 0};
+                sums = q % 2 == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, sums, 4, 4, 0, (int)sa[i][q / 2], 0, (int)sb[i][q / 2])
+                                  : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, sums, 4, 4, 2, (int)sa[i][q / 2], 2, (int)sb[i][q / 2]);
+            }
+    }
+#pragma unroll
+    for (int q = 0; q < 16; ++q) parts[wave][(q / 4 * 8 + h * 4 + q % 4) * 32 + r] = sums[q];
+    __syncthreads();
+    for (int at = threadIdx.x; at < (int)g.m * 32; at += kFewWaves * kWave) {
+        const int64_t row = at / 32, col = col0 + at % 32;
         float sum = 0.0f;
-        if (col < n)
-            for (int64_t s = 0; s < n_parts; ++s) sum += parts[(s * m + row) * n + col];
-        out[row * ldo + col] = (T)sum;
+#pragma unroll
+        for (int w = 0; w < kFewWaves; ++w) sum += parts[w][at];
+        if (col < g.written) ((T *)g.out)[(blockIdx.y * g.m + row) * g.ldo + col] = col < g.n ? (T)sum : (T)0.0f;
     }
 }
 
+// The splits' sums, in order; columns from n to `written` are zeros.  A workgroup of 64 columns and four rows.
+template <typename T>
+__global__ __launch_bounds__(kBlock) void mx4_join_kernel(const float *parts, int n_parts, int64_t m, int64_t n, int64_t written, T *out, int64_t ldo)
+{
+    constexpr int kAtOnce = 8;
+    const int64_t col = (int64_t)blockIdx.x * kWave + threadIdx.x % kWave;
+    if (col >= written) return;
+    for (int64_t row = (int64_t)blockIdx.y * kWavesPerBlock + threadIdx.x / kWave; row < m; row += (int64_t)gridDim.y * kWavesPerBlock) {
+        const float *from = parts + row * n + min(col, n - 1);
+        float sum = 0.0f;
+        for (int s = 0; s < n_parts; s += kAtOnce) {
+            float v[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) v[k] = from[min(s + k, n_parts - 1) * m * n];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k)
+                if (s + k < n_parts) sum += v[k];
+        }
+        out[row * ldo + col] = col < n ? (T)sum : (T)0.0f;
+    }
+}
+
+enum MulTile { FEW_ROWS, TILE_64_64, TILE_128_64, TILE_128_64_DEEP, TILE_128_128, TILE_256_256 };
+
 struct MulShape {
-    int tile;
+    MulTile tile;
     int64_t tiles_m, tiles_n, steps, splits, steps_per_split, bytes;
 };
 
+// Large tiles read less and small ones overlap more: a workgroup of 256 x 256 fills a CU's LDS by itself, so that nothing runs while it begins and ends, and two of
+// 128 x 128 or four of 128 x 64 share one.  us for 8192 x 8192 outputs, k = 1024, 2048, 4096, 8192: 256 x 256 91, 121, 184, 306; 128 x 128 75, 115, 189, 329;
+// 128 x 64 70, 122, 203, 376.  2048 x 2048, k = 2048, 256 tiles of 128 x 128: 14.7 against 13.0 with 128 x 64.
+// k is split where tiles of 64 x 64 leave half of the CUs idle, in parts of at least eight steps, to about 480 workgroups (256 x 300 outputs, k = 196 000: 12, 24,
+// 50 parts 29, 26, 34 us); from 25 such tiles on, tiles of 128 x 64 with one more step under way (256 x 602, k = 306 000: 70 us, 64 x 64 more than 78).
 MulShape mul_shape(int64_t m, int64_t n, int64_t k)
 {
     MulShape s{};
-    auto tiles = [&](int t) {
+    auto tiles = [&](MulTile t, int64_t rows, int64_t cols) {
         s.tile = t;
-        s.tiles_m = (m + t - 1) / t;
-        s.tiles_n = (n + t - 1) / t;
+        s.tiles_m = (m + rows - 1) / rows;
+        s.tiles_n = (n + cols - 1) / cols;
         return s.tiles_m * s.tiles_n;
     };
-    if (tiles(256) < 256 && tiles(128) < 256) tiles(64);
-    const int64_t blocks = s.tiles_m * s.tiles_n;
     s.steps = (mx_chunks(k) + kStepChunks - 1) / kStepChunks;
-    int64_t splits = blocks >= 256 || blocks == 0 ? 1 : 512 / blocks;
-    if (splits > s.steps / 2) splits = s.steps / 2;
-    if (splits < 1) splits = 1;
-    s.steps_per_split = (s.steps + splits - 1) / splits;
-    s.splits = s.steps ? (s.steps + s.steps_per_split - 1) / s.steps_per_split : 1;
-    s.bytes = s.splits > 1 ? (s.splits * m * n * 4 + 255) / 256 * 256 : 0;
+    s.splits = 1;
+    s.steps_per_split = s.steps;
+    auto split = [&](int64_t splits) {
+        if (splits < 2) return;
+        s.steps_per_split = (s.steps + splits - 1) / splits;
+        s.splits = (s.steps + s.steps_per_split - 1) / s.steps_per_split;
+        s.bytes = s.splits > 1 ? (s.splits * m * n * 4 + 255) / 256 * 256 : 0;
+    };
+    if (m == 0 || n == 0) return s;
+    if (m <= kFewRows) {
+        const int64_t blocks = tiles(FEW_ROWS, kFewRows, 32), most = s.steps / (4 * kFewWaves);
+        split(256 / blocks < most ? 256 / blocks : most);
+        return s;
+    }
+    if (s.steps >= 12 && tiles(TILE_256_256, 256, 256) >= 512) return s;
+    if (s.steps >= 6 && tiles(TILE_128_128, 128, 128) >= 512) return s;
+    if (tiles(TILE_128_64, 128, 64) >= 256) return s;
+    const int64_t small = tiles(TILE_64_64, 64, 64);
+    if (small >= 128 || s.steps < 16) return s;
+    const int64_t blocks = small >= 25 ? tiles(TILE_128_64_DEEP, 128, 64) : small;
+    split(480 / blocks < s.steps / 8 ? 480 / blocks : s.steps / 8);
     return s;
 }
 
@@ -245,9 +335,14 @@ template <typename T>
 void launch_tiles(const MulArgs &g, const MulShape &s, hipStream_t st)
 {
     const uint32_t blocks = (uint32_t)tile_blocks(s.tiles_m * s.tiles_n, s.splits);
-    if (s.tile == 256) mx4_matmul_kernel<T, 256, 256, 2><<<blocks, kBlock, 0, st>>>(g);
-    else if (s.tile == 128) mx4_matmul_kernel<T, 128, 128, 2><<<blocks, kBlock, 0, st>>>(g);
-    else               mx4_matmul_kernel<T, 64, 64, 4><<<blocks, kBlock, 0, st>>>(g);
+    switch (s.tile) {
+        case FEW_ROWS:         mx4_few_rows_kernel<T><<<dim3((uint32_t)((g.written + 31) / 32), (uint32_t)s.splits), kFewWaves * kWave, 0, st>>>(g); break;
+        case TILE_64_64:       mx4_matmul_kernel<T, 64, 64, 4><<<blocks, kBlock, 0, st>>>(g); break;
+        case TILE_128_64:      mx4_matmul_kernel<T, 128, 64, 2><<<blocks, kBlock, 0, st>>>(g); break;
+        case TILE_128_64_DEEP: mx4_matmul_kernel<T, 128, 64, 3><<<blocks, kBlock, 0, st>>>(g); break;
+        case TILE_128_128:     mx4_matmul_kernel<T, 128, 128, 2><<<blocks, kBlock, 0, st>>>(g); break;
+        case TILE_256_256:     mx4_matmul_kernel<T, 256, 256, 2><<<blocks, kBlock, 0, st>>>(g); break;
+    }
 }
 
 int check_sizes(int64_t m, int64_t n, int64_t k)
@@ -294,10 +389,10 @@ extern "C" int adaqp_mx4_matmul(const uint8_t *a_codes_dev, const uint8_t *a_sca
         g.ldo = n;
         launch_tiles<float>(g, s, st);
         ADAQP_HIP_TRY(hipGetLastError());
-        const int64_t blocks = (m * written + kBlock - 1) / kBlock;
-        const uint32_t grid = (uint32_t)(blocks < 4096 ? blocks : 4096);
-        if (type == ADAQP_F32) mx4_join_kernel<float><<<grid, kBlock, 0, st>>>((const float *)workspace_dev, s.splits, m, n, written, (float *)out_dev, ldo);
-        else                   mx4_join_kernel<__bf16><<<grid, kBlock, 0, st>>>((const float *)workspace_dev, s.splits, m, n, written, (__bf16 *)out_dev, ldo);
+        const int64_t rows = (m + kWavesPerBlock - 1) / kWavesPerBlock;
+        const dim3 grid((uint32_t)((written + kWave - 1) / kWave), (uint32_t)(rows < 65535 ? rows : 65535));
+        if (type == ADAQP_F32) mx4_join_kernel<float><<<grid, kBlock, 0, st>>>((const float *)workspace_dev, (int)s.splits, m, n, written, (float *)out_dev, ldo);
+        else                   mx4_join_kernel<__bf16><<<grid, kBlock, 0, st>>>((const float *)workspace_dev, (int)s.splits, m, n, written, (__bf16 *)out_dev, ldo);
     } else if (type == ADAQP_F32) launch_tiles<float>(g, s, st);
     else                          launch_tiles<__bf16>(g, s, st);
     ADAQP_HIP_TRY(hipGetLastError());
