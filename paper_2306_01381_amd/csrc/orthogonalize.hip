@@ -18,10 +18,12 @@ namespace {
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
 typedef float sums16 __attribute__((ext_vector_type(16)));
 
 constexpr int kPad = 64;                            // rows and columns of the held matrices are multiples
-constexpr int kNormBlocks = 256;                    // of a matrix, at most
+constexpr int kNormBlocks = 512;                    // of a matrix, at most
+constexpr int kNormRun = 8 * kBlock;                // columns
 constexpr int kMostPower = 14;
 constexpr int64_t kMostSize = (int64_t)1 << 20;
 
@@ -43,23 +45,34 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
-// Sums of squares of a share of each matrix: blocks [x] of matrix [y], runs of kBlock columns of a row.
+// Sums of squares of a share of each matrix: blocks [x] of matrix [y], runs of eight columns a thread.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void update_norm_kernel(const T *g, int64_t ldg, int64_t stride, int64_t n_rows, int64_t n_cols, double *partial)
 {
     __shared__ double lds[kWavesPerBlock];
     g += blockIdx.y * stride;
-    const uint32_t runs = (uint32_t)((n_cols + kBlock - 1) / kBlock);
+    const uint32_t runs = (uint32_t)((n_cols + kNormRun - 1) / kNormRun);
     const int64_t total = n_rows * runs;
     double sum = 0.0;
-#pragma unroll 4
     for (int64_t at = blockIdx.x; at < total; at += gridDim.x) {
-        const uint32_t row = (uint32_t)((uint64_t)at / runs), col = ((uint32_t)at - row * runs) * kBlock + threadIdx.x;
-        const double v = col < n_cols ? (double)(float)g[row * ldg + col] : 0.0;
-        sum = fma(v, v, sum);
+        const int64_t row = at / runs, col = (at - row * runs) * kNormRun + threadIdx.x;
+        float v[kNormRun / kBlock];
+#pragma unroll
+        for (int k = 0; k < kNormRun / kBlock; ++k) v[k] = (float)g[row * ldg + min(col + k * kBlock, n_cols - 1)];
+#pragma unroll
+        for (int k = 0; k < kNormRun / kBlock; ++k)
+            if (col + k * kBlock < n_cols) sum = fma((double)v[k], (double)v[k], sum);
     }
     sum = block_sum(sum, lds);
     if (threadIdx.x == 0) partial[blockIdx.y * gridDim.x + blockIdx.x] = sum;
+}
+
+// A matrix's sum of squares, by all threads of a workgroup.
+__device__ __forceinline__ double norm_square(const double *partial, int n_partial, double *lds)
+{
+    static_assert(kNormBlocks <= 2 * kBlock, "two partial sums a thread");
+    const int t = threadIdx.x;
+    return block_sum((t < n_partial ? partial[t] : 0.0) + (t + kBlock < n_partial ? partial[t + kBlock] : 0.0), lds);
 }
 
 // G / (norm + eps) in units of 2^-power as held matrices: as it lies (`same`) and transposed (`other`), zeros up to the padded sizes.  A workgroup takes 64 x 64.
@@ -82,7 +95,7 @@ __global__ __launch_bounds__(kBlock) void update_split_kernel(const T *g, int64_
         const int64_t row = row0 + r0 + i * (kBlock / kPad), col = col0 + c;
         v[i] = row < n_rows && col < n_cols ? (float)g[row * ldg + col] : 0.0f;
     }
-    const double total = block_sum((int)threadIdx.x < n_partial ? partial[blockIdx.z * n_partial + threadIdx.x] : 0.0, lds);
+    const double total = norm_square(partial + blockIdx.z * n_partial, n_partial, lds);
     const double scale = ldexp(1.0 / (sqrt(total) + eps), power);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -121,153 +134,374 @@ struct ProductArgs {
     void *out;                                      // LAST: D itself
     int64_t ldo, stride_o, out_rows, out_cols, written;
     int64_t tiles_r, tiles_c;
+    int parts;                                      // cuts of the lines
+    float *sums;                                    // of parts, more than one: [matrix][part][tile][a workgroup's registers]
 };
 
-template <Product KIND, typename T, int TILE, int STAGES>
+// Tiles below and on the diagonal, row by row.
+__device__ __forceinline__ void triangle_tile(uint32_t block, int64_t &row, int64_t &col)
+{
+    row = (int64_t)((sqrtf(8.0f * block + 1.0f) - 1.0f) * 0.5f);
+    while (row * (row + 1) / 2 > block) --row;
+    while ((row + 1) * (row + 2) / 2 <= block) ++row;
+    col = block - row * (row + 1) / 2;
+}
+
+// The same in squares of 4 x 4 tiles: `block` of a square's 16, squares below and on the diagonal row by row.  Workgroups of tiles that are not there (beyond the
+// diagonal, or the edge) have nothing to do.
+constexpr int kSquare = 4;
+
+__host__ __device__ inline int64_t squares_of(int64_t tiles)
+{
+    const int64_t n = (tiles + kSquare - 1) / kSquare;
+    return n * (n + 1) / 2;
+}
+
+// v in the units of POLY's sums: b A + c A A + a I, of which `p` holds A.
+__device__ __forceinline__ float polynomial(const ProductArgs &g, const uint8_t *p, int64_t row, int64_t col, float v)
+{
+    const uint8_t *from = p + held_at(row, col, g.pitch);
+    const float a = (float)*reinterpret_cast<const _Float16 *>(from) + (float)*reinterpret_cast<const _Float16 *>(from + 64);
+    return fmaf(g.linear, a, v) + (row == col ? g.diagonal : 0.0f);
+}
+
+constexpr int kSmallTile = 32, kSmallWaves = 8;
+
+// Few tiles: 32 x 32 each, whose eight waves share the lines (w, w + 8, ...) and read them into registers, all at once where there are no more than 16.
+// A product of 256 x 256 x 256 then waits for memory once.
+template <Product KIND, typename T>
+__global__ __launch_bounds__(kSmallWaves * kWave) void update_small_product_kernel(ProductArgs g)
+{
+    constexpr bool kSymmetric = KIND == GRAM || KIND == POLY;
+    constexpr int kLines = 2;                       // under way
+    __shared__ float parts[kSmallWaves][kSmallTile * kSmallTile];
+    __shared__ float tile[kSmallTile][kSmallTile + 1];
+    int64_t tr, tc;
+    if (kSymmetric) triangle_tile(blockIdx.x, tr, tc);
+    else {
+        tr = blockIdx.x / g.tiles_c;
+        tc = blockIdx.x % g.tiles_c;
+    }
+    const uint8_t *p = g.p + blockIdx.y * g.bytes_p, *q = g.q + blockIdx.y * g.bytes_q;
+    const int64_t row0 = tr * kSmallTile, col0 = tc * kSmallTile;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+    const uint8_t *from_p = p + (row0 + r) * g.pitch + h * 16, *from_q = q + (col0 + r) * g.pitch + h * 16;
+    sums16 sums;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sums[e] = 0.0f;
+    for (int line = wave; line < (int)g.lines; line += kSmallWaves * kLines) {
+        half8 x[kLines][4], y[kLines][4];           // hi of the two halves of a line, lo of them
+#pragma unroll
+        for (int i = 0; i < kLines; ++i) {
+            const int64_t at = (int64_t)min(line + i * kSmallWaves, (int)g.lines - 1) * kLine;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[i][k] = *reinterpret_cast<const half8 *>(from_p + at + k * 32);
+                y[i][k] = *reinterpret_cast<const half8 *>(from_q + at + k * 32);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kLines; ++i) {
+            if (line + i * kSmallWaves >= (int)g.lines) break;
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][2 + k], y[i][k], sums, 0, 0, 0);
+                sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][k], y[i][2 + k], sums, 0, 0, 0);
+                sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][k], y[i][k], sums, 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) parts[wave][(e / 4 * 8 + h * 4 + e % 4) * kSmallTile + r] = sums[e];
+    __syncthreads();
+    // two neighbouring columns a thread, then two rows
+    const int major = threadIdx.x / 16, minor = threadIdx.x % 16 * 2;
+    float v[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < kSmallWaves; ++w) {
+        v[0] += parts[w][major * kSmallTile + minor];
+        v[1] += parts[w][major * kSmallTile + minor + 1];
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        v[k] *= g.scale;
+        if (KIND == POLY) v[k] = polynomial(g, p, row0 + major, col0 + minor + k, v[k]);
+    }
+    if constexpr (KIND == LAST) {
+        T *out = (T *)g.out + blockIdx.y * g.stride_o;
+        const int64_t row = row0 + major;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int64_t col = col0 + minor + k;
+            if (row < g.out_rows && col < g.written) out[row * g.ldo + col] = col < g.out_cols ? (T)v[k] : (T)0.0f;
+        }
+    } else {
+        auto store = [](uint8_t *to, float first, float second) {
+            half2 hi, lo;
+            _Float16 a, b;
+            split(first, a, b);
+            hi[0] = a;
+            lo[0] = b;
+            split(second, a, b);
+            hi[1] = a;
+            lo[1] = b;
+            *reinterpret_cast<half2 *>(to) = hi;
+            *reinterpret_cast<half2 *>(to + 64) = lo;
+        };
+        store(g.same + blockIdx.y * g.bytes_d + held_at(row0 + major, col0 + minor, g.pitch_same), v[0], v[1]);
+        if (kSymmetric && tr == tc) return;
+        tile[major][minor] = v[0];
+        tile[major][minor + 1] = v[1];
+        __syncthreads();
+        store(g.other + blockIdx.y * g.bytes_d + held_at(col0 + major, row0 + minor, g.pitch_other), tile[minor][major], tile[minor + 1][major]);
+    }
+}
+
+// Which tile, and which cut of the lines; false: none.  XCDs get neighbouring tiles.
+template <bool SYMMETRIC>
+__device__ __forceinline__ bool product_tile(const ProductArgs &g, int64_t &tr, int64_t &tc, int &part)
+{
+    if (SYMMETRIC) {
+        const uint32_t at = xcd_neighbour(blockIdx.x, gridDim.x), in_square = at % (kSquare * kSquare), square = at / (kSquare * kSquare);
+        int64_t row, col;
+        triangle_tile(square / g.parts, row, col);
+        part = (int)(square % g.parts);
+        tr = row * kSquare + in_square / kSquare;
+        tc = col * kSquare + in_square % kSquare;
+        return tr < g.tiles_r && tc <= tr;
+    }
+    const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_r, (uint32_t)g.tiles_c, 1);
+    tr = place.row;
+    tc = place.col;
+    part = 0;
+    return place.part >= 0;
+}
+
+// A wave's 32 x 32 sums on their way out, in the LDS.
+constexpr int kSheetPitch = 36;
+struct Sheet { float v[32 * kSheetPitch]; };
+
+// 16 neighbouring columns of a held row, from a multiple of 16 on.
+__device__ __forceinline__ void store_held(uint8_t *to, const float (&v)[16])
+{
+    half8 hi[2], lo[2];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        _Float16 a, b;
+        split(v[k], a, b);
+        hi[k / 8][k % 8] = a;
+        lo[k / 8][k % 8] = b;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        *reinterpret_cast<half8 *>(to + k * 16) = hi[k];
+        *reinterpret_cast<half8 *>(to + 64 + k * 16) = lo[k];
+    }
+}
+
+// Stores what a wave's 32 x 32 sums at (row0, col0) of D say.  Held matrices through the sheet, so that a lane has 16 neighbours of a row, then 16 of a column: stored
+// from the sums' own places, two bytes and four rows a lane, a product of 4096 x 2048 x 2048 took 31 of its 104 us for it.
+template <Product KIND, typename T>
+__device__ __forceinline__ void store_sums(const ProductArgs &g, const uint8_t *p, int64_t row0, int64_t col0, bool on_diagonal, const sums16 &sums, Sheet &sheet)
+{
+    constexpr bool kSymmetric = KIND == GRAM || KIND == POLY;
+    const int lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+    if (row0 >= g.rows || col0 >= g.cols) return;   // the sizes are multiples of 64
+    if constexpr (KIND == LAST) {
+        T *out = (T *)g.out + blockIdx.y * g.stride_o + row0 * g.ldo + col0 + r;
+        const int rows = (int)min(g.out_rows - row0, (int64_t)32), cols = (int)min(g.out_cols - col0, (int64_t)32), written = (int)min(g.written - col0, (int64_t)32);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const int row = e / 4 * 8 + h * 4 + e % 4;
+            if (row < rows && r < written) out[row * g.ldo] = r < cols ? (T)(sums[e] * g.scale) : (T)0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sheet.v[(e / 4 * 8 + h * 4 + e % 4) * kSheetPitch + r] = sums[e] * g.scale;
+        const int line = lane / 2, part = lane % 2 * 16;
+        float v[16];
+#pragma unroll
+        for (int k = 0; k < 16; k += 4) {
+            const float4 w = *reinterpret_cast<const float4 *>(&sheet.v[line * kSheetPitch + part + k]);
+            v[k] = w.x;
+            v[k + 1] = w.y;
+            v[k + 2] = w.z;
+            v[k + 3] = w.w;
+        }
+        if (KIND == POLY) {
+            const uint8_t *from = p + held_at(row0 + line, col0 + part, g.pitch);
+            half8 hi[2], lo[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                hi[k] = *reinterpret_cast<const half8 *>(from + k * 16);
+                lo[k] = *reinterpret_cast<const half8 *>(from + 64 + k * 16);
+            }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                v[k] = fmaf(g.linear, (float)hi[k / 8][k % 8] + (float)lo[k / 8][k % 8], v[k]) + (row0 + line == col0 + part + k ? g.diagonal : 0.0f);
+                sheet.v[line * kSheetPitch + part + k] = v[k];
+            }
+        }
+        store_held(g.same + blockIdx.y * g.bytes_d + held_at(row0 + line, col0 + part, g.pitch_same), v);
+        if (kSymmetric && on_diagonal) return;      // of a tile on the diagonal both halves are there
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = sheet.v[(part + k) * kSheetPitch + line];
+        store_held(g.other + blockIdx.y * g.bytes_d + held_at(col0 + line, row0 + part, g.pitch_other), v);
+    }
+}
+
+// Tiles of TR x TC, a quarter each wave.
+template <Product KIND, typename T, int TR, int TC, int STAGES>
 __global__ __launch_bounds__(kBlock) void update_product_kernel(ProductArgs g)
 {
     constexpr bool kSymmetric = KIND == GRAM || KIND == POLY;
-    constexpr int F = TILE / 64;                    // 32 x 32 parts of a wave, both ways
-    __shared__ struct { uint8_t p[TILE * kLine], q[TILE * kLine]; } stage[STAGES];
+    constexpr int FR = TR / 64, FC = TC / 64;       // 32 x 32 parts of a wave
+    struct Stage { uint8_t p[TR * kLine], q[TC * kLine]; };
+    __shared__ __align__(16) uint8_t lds[sizeof(Stage) * STAGES];
+    static_assert(sizeof(lds) >= kWavesPerBlock * sizeof(Sheet), "the sheets lie where the operands were");
+    Stage *stage = reinterpret_cast<Stage *>(lds);
     int64_t tr, tc;
-    if (kSymmetric) {                               // tiles below and on the diagonal, row by row
-        tr = (int64_t)((sqrtf(8.0f * blockIdx.x + 1.0f) - 1.0f) * 0.5f);
-        while (tr * (tr + 1) / 2 > blockIdx.x) --tr;
-        while ((tr + 1) * (tr + 2) / 2 <= blockIdx.x) ++tr;
-        tc = blockIdx.x - tr * (tr + 1) / 2;
-    } else {
-        const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_r, (uint32_t)g.tiles_c, 1);
-        if (place.part < 0) return;
-        tr = place.row;
-        tc = place.col;
-    }
+    int part;
+    if (!product_tile<kSymmetric>(g, tr, tc, part)) return;
     const uint8_t *p = g.p + blockIdx.y * g.bytes_p, *q = g.q + blockIdx.y * g.bytes_q;
-    const int64_t row0 = tr * TILE, col0 = tc * TILE, pitch = g.pitch;
+    const int64_t row0 = tr * TR, col0 = tc * TC, pitch = g.pitch;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
-    const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
+    const int wr = wave / 2 * (TR / 2), wc = wave % 2 * (TC / 2);
 
-    sums16 sums[F][F];
+    sums16 sums[FR][FC];
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < FR; ++i)
 #pragma unroll
-        for (int j = 0; j < F; ++j)
+        for (int j = 0; j < FC; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e) sums[i][j][e] = 0.0f;
 
-    const TileLoads<TILE> of_p(row0, g.rows, pitch), of_q(col0, g.cols, pitch);
-    constexpr int kLoads = 2 * TileLoads<TILE>::kLoads;
-    const uint8_t *from_p = p + row0 * pitch, *from_q = q + col0 * pitch;
+    const TileLoads<TR> of_p(row0, g.rows, pitch);
+    const TileLoads<TC> of_q(col0, g.cols, pitch);
+    constexpr int kLoadsP = TileLoads<TR>::kLoads, kLoads = kLoadsP + TileLoads<TC>::kLoads;
+    const int per_part = (int)((g.lines + g.parts - 1) / g.parts), begin = part * per_part, lines = min(per_part, (int)g.lines - begin);
+    const uint8_t *from_p = p + row0 * pitch + (int64_t)begin * kLine, *from_q = q + col0 * pitch + (int64_t)begin * kLine;
     // Load i of a line of both operands.
     auto load = [&](int i, int line, const auto &s) {
-        if (i < kLoads / 2) of_p.template load<false>(i, from_p + (int64_t)line * kLine, TileLoads<TILE>::place(s.p));
-        else                of_q.template load<false>(i - kLoads / 2, from_q + (int64_t)line * kLine, TileLoads<TILE>::place(s.q));
+        if (i < kLoadsP) of_p.template load<false>(i, from_p + (int64_t)line * kLine, TileLoads<TR>::place(s.p));
+        else             of_q.template load<false>(i - kLoadsP, from_q + (int64_t)line * kLine, TileLoads<TC>::place(s.q));
     };
     // The operands of half a line, 16 columns: read from the LDS while the half before is multiplied.
-    struct Half { half8 ph[F], pl[F], qh[F], ql[F]; } half[2];
+    struct Half { half8 ph[FR], pl[FR], qh[FC], ql[FC]; } half[2];
     auto read = [&](const auto &s, int k, Half &to) {
 #pragma unroll
-        for (int i = 0; i < F; ++i) {
+        for (int i = 0; i < FR; ++i) {
             to.ph[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, k * 2 + h));
             to.pl[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, 4 + k * 2 + h));
-            to.qh[i] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + i * 32 + r, k * 2 + h));
-            to.ql[i] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + i * 32 + r, 4 + k * 2 + h));
+        }
+#pragma unroll
+        for (int j = 0; j < FC; ++j) {
+            to.qh[j] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + j * 32 + r, k * 2 + h));
+            to.ql[j] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + j * 32 + r, 4 + k * 2 + h));
         }
     };
-    // `between(p)` is done behind product p of the half's 3 F F.
+    // `between(i)` is done behind product i of the half's 3 FR FC.
     auto multiply = [&](const Half &f, auto between) {
 #pragma unroll
         for (int w = 0; w < 3; ++w)                 // the small ones first
 #pragma unroll
-            for (int i = 0; i < F; ++i)
+            for (int i = 0; i < FR; ++i)
 #pragma unroll
-                for (int j = 0; j < F; ++j) {
+                for (int j = 0; j < FC; ++j) {
                     sums[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.pl[i] : f.ph[i], w == 1 ? f.ql[j] : f.qh[j], sums[i][j], 0, 0, 0);
-                    between((w * F + i) * F + j);
+                    between((w * FR + i) * FC + j);
                 }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto nothing = [](int) {};
 
     // Up to STAGES lines are under way.  A line's second half is multiplied behind the barrier after which the next line is in the LDS and its own buffer
-    // free, and the loads into that buffer are issued between its products.  No branches: across one the compiler would take products to the other side
-    // of the barrier.
-    const int lines = (int)g.lines;
+    // free; the loads into that buffer are spread over that half's products and those of the next line's first half.  No branches: across one the compiler
+    // would take products to the other side of the barrier.
+    constexpr int kProducts = 3 * FR * FC, kFirst = kLoads / 2;         // loads behind the products of a second half
 #pragma unroll
     for (int s = 0; s < STAGES; ++s)
         if (s < lines)
 #pragma unroll
-            for (int l = 0; l < kLoads; ++l) load(l, s, stage[s]);
-    if (lines >= STAGES) arrived<kLoads * (STAGES - 1)>();
+            for (int l = 0; l < (s < STAGES - 1 ? kLoads : kFirst); ++l) load(l, s, stage[s]);
+    if (lines >= STAGES) arrived<kLoads * (STAGES - 2) + kFirst>();
     else                 arrived<0>();
     read(stage[0], 0, half[0]);
-    int now = 0;
-    auto one = [&](int line, auto more) {
-        constexpr bool kMore = decltype(more)::value;
-        const auto &s = stage[now];
+    int now = 0, before = STAGES - 1;
+    auto one = [&](int line, auto pending, auto more) {
+        constexpr bool kPending = decltype(pending)::value, kMore = decltype(more)::value;
+        const Stage &s = stage[now], &last = stage[before];
+        before = now;
         now = now + 1 == STAGES ? 0 : now + 1;
         read(s, 1, half[1]);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(half[0], nothing);
-        arrived<kMore ? kLoads * (STAGES - 2) : 0>();
+        multiply(half[0], [&](int i) {
+            if constexpr (kPending) {
+#pragma unroll
+                for (int l = kFirst + i * (kLoads - kFirst) / kProducts; l < kFirst + (i + 1) * (kLoads - kFirst) / kProducts; ++l) load(l, line - 1 + STAGES, last);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+        arrived<kPending ? kLoads * (STAGES - 2) : 0>();
         read(stage[now], 0, half[0]);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(half[1], [&](int p) {
+        multiply(half[1], [&](int i) {
             if constexpr (kMore) {
 #pragma unroll
-                for (int l = p * kLoads / (3 * F * F); l < (p + 1) * kLoads / (3 * F * F); ++l) load(l, line + STAGES, s);
+                for (int l = i * kFirst / kProducts; l < (i + 1) * kFirst / kProducts; ++l) load(l, line + STAGES, s);
                 __builtin_amdgcn_sched_barrier(0);
             }
         });
     };
     int line = 0;
-    for (; line + STAGES < lines; ++line) one(line, std::true_type());
-    for (; line < lines; ++line) one(line, std::false_type());
+    for (; line + STAGES < lines; ++line) one(line, std::true_type(), std::true_type());
+    if (lines >= STAGES) one(line++, std::true_type(), std::false_type());
+    for (; line < lines; ++line) one(line, std::false_type(), std::false_type());
 
-    uint8_t *same = g.same + blockIdx.y * g.bytes_d, *other = g.other + blockIdx.y * g.bytes_d;
+    if (kSymmetric && g.parts > 1) {
+        float4 *to = reinterpret_cast<float4 *>(g.sums + ((blockIdx.y * g.parts + part) * (g.tiles_r * (g.tiles_r + 1) / 2) + tr * (tr + 1) / 2 + tc) * (TR * TC));
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+        for (int i = 0; i < FR; ++i)
 #pragma unroll
-        for (int j = 0; j < F; ++j) {
-            const int64_t col = col0 + wc + j * 32 + r;
+            for (int j = 0; j < FC; ++j)
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const int64_t row = row0 + wr + i * 32 + e / 4 * 8 + h * 4;
-                if (row >= g.rows || col >= g.cols) continue;
-                float v[4];
+                for (int e = 0; e < 16; e += 4)
+                    to[((i * FC + j) * 4 + e / 4) * kBlock + threadIdx.x] = make_float4(sums[i][j][e], sums[i][j][e + 1], sums[i][j][e + 2], sums[i][j][e + 3]);
+        return;
+    }
+    arrived<0>();                                   // nobody reads the operands any more
+    Sheet &sheet = reinterpret_cast<Sheet *>(lds)[wave];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    v[k] = sums[i][j][e + k] * g.scale;
-                    if (KIND == POLY) {
-                        const uint8_t *from = p + held_at(row + k, col, pitch);
-                        const float a = (float)*reinterpret_cast<const _Float16 *>(from) + (float)*reinterpret_cast<const _Float16 *>(from + 64);
-                        v[k] = fmaf(g.linear, a, v[k]) + (row + k == col ? g.diagonal : 0.0f);
-                    }
-                }
-                if constexpr (KIND == LAST) {
-                    T *out = (T *)g.out + blockIdx.y * g.stride_o;
+    for (int i = 0; i < FR; ++i)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (row + k < g.out_rows && col < g.written) out[(row + k) * g.ldo + col] = col < g.out_cols ? (T)v[k] : (T)0.0f;
-                } else {
-                    half4 hi, lo;
+        for (int j = 0; j < FC; ++j) store_sums<KIND, T>(g, p, row0 + wr + i * 32, col0 + wc + j * 32, tr == tc, sums[i][j], sheet);
+}
+
+// A symmetric product whose lines were cut: the parts' sums, in order, and what is made of them.  A workgroup takes a part (i, j) = blockIdx.z of each wave's.
+template <Product KIND, int TILE>
+__global__ __launch_bounds__(kBlock) void update_join_kernel(ProductArgs g)
+{
+    constexpr int F = TILE / 64;
+    __shared__ Sheet sheets[kWavesPerBlock];
+    int64_t tr, tc;
+    triangle_tile(blockIdx.x, tr, tc);
+    const int wave = threadIdx.x / kWave, i = blockIdx.z / F, j = blockIdx.z % F;
+    const int64_t tiles = g.tiles_r * (g.tiles_r + 1) / 2;
+    const float4 *from = reinterpret_cast<const float4 *>(g.sums + (blockIdx.y * g.parts * tiles + blockIdx.x) * (TILE * TILE)) + blockIdx.z * 4 * kBlock + threadIdx.x;
+    sums16 sums;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        _Float16 a, b;
-                        split(v[k], a, b);
-                        hi[k] = a;
-                        lo[k] = b;
-                        uint8_t *to = same + held_at(row + k, col, g.pitch_same);
-                        *reinterpret_cast<_Float16 *>(to) = a;
-                        *reinterpret_cast<_Float16 *>(to + 64) = b;
-                    }
-                    if (!kSymmetric || tr != tc) {  // of a tile on the diagonal both halves are there
-                        uint8_t *to = other + held_at(col, row, g.pitch_other);
-                        *reinterpret_cast<half4 *>(to) = hi;
-                        *reinterpret_cast<half4 *>(to + 64) = lo;
-                    }
-                }
-            }
+    for (int e = 0; e < 16; ++e) sums[e] = 0.0f;
+    for (int part = 0; part < g.parts; ++part, from += tiles * (TILE * TILE) / 4) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const float4 v = from[e / 4 * kBlock];
+            sums[e] += v.x;
+            sums[e + 1] += v.y;
+            sums[e + 2] += v.z;
+            sums[e + 3] += v.w;
         }
+    }
+    store_sums<KIND, float>(g, g.p + blockIdx.y * g.bytes_p, tr * TILE + wave / 2 * (TILE / 2) + i * 32, tc * TILE + wave % 2 * (TILE / 2) + j * 32, tr == tc, sums,
+                              sheets[wave]);
 }
 
 template <typename T>
@@ -275,7 +509,7 @@ __global__ __launch_bounds__(kBlock) void update_scale_kernel(const T *g, int64_
                                                               int n_partial, double eps, T *out, int64_t ldo, int64_t stride_o, int64_t written)
 {
     __shared__ double lds[kWavesPerBlock];
-    const double total = block_sum((int)threadIdx.x < n_partial ? partial[blockIdx.y * n_partial + threadIdx.x] : 0.0, lds);
+    const double total = norm_square(partial + blockIdx.y * n_partial, n_partial, lds);
     const double scale = 1.0 / (sqrt(total) + eps);
     g += blockIdx.y * stride;
     out += blockIdx.y * stride_o;
@@ -295,8 +529,21 @@ struct UpdateLayout {
     int64_t n, m;                                   // padded, n of the smaller
     int64_t big, small;                             // bytes of X and of A
     int64_t norm_blocks;
-    int64_t partial_at, x_at, a_at, q_at, bytes;    // X, its transpose, both again for the next step
+    int parts_m, parts_n;                           // cuts of the lines of symmetric products over m and over n, tiles of 128 x 128
+    int64_t partial_at, x_at, a_at, q_at, sums_at, bytes;       // X, its transpose, both again for the next step
 };
+
+// Cuts of the lines of a symmetric product of n x n: two tiles of 128 x 128 share a CU, and with at least kCutTiles of them there are enough for tiles of that size to
+// pay, but fewer than there is room for.
+constexpr int kCutTiles = 100, kRoom = 512, kLeastLines = 16;
+
+int update_parts(int64_t n, int64_t lines, int64_t n_matrices)
+{
+    const int64_t t = (n + 127) / 128, tiles = t * (t + 1) / 2 * n_matrices;
+    if (tiles < kCutTiles || 2 * tiles > kRoom) return 1;
+    const int64_t parts = kRoom / tiles < lines / kLeastLines ? kRoom / tiles : lines / kLeastLines;
+    return parts < 1 ? 1 : (int)((lines + (lines + parts - 1) / parts - 1) / ((lines + parts - 1) / parts));
+}
 
 UpdateLayout update_layout(int32_t n_matrices, int64_t n_rows, int64_t n_cols)
 {
@@ -307,13 +554,17 @@ UpdateLayout update_layout(int32_t n_matrices, int64_t n_rows, int64_t n_cols)
     const int64_t of_x = u.n * held_pitch(u.m), of_xt = u.m * held_pitch(u.n);
     u.big = of_x > of_xt ? of_x : of_xt;
     u.small = u.n * held_pitch(u.n);
-    u.norm_blocks = (n_rows * ((n_cols + kBlock - 1) / kBlock) + 3) / 4;
+    u.norm_blocks = n_rows * ((n_cols + kNormRun - 1) / kNormRun);
     if (u.norm_blocks > kNormBlocks) u.norm_blocks = kNormBlocks;
     u.partial_at = 0;
     u.x_at = (n_matrices * u.norm_blocks * 8 + 255) / 256 * 256;
     u.a_at = u.x_at + 4 * n_matrices * u.big;
     u.q_at = u.a_at + n_matrices * u.small;
-    u.bytes = u.q_at + n_matrices * u.small;
+    u.sums_at = u.q_at + n_matrices * u.small;
+    u.parts_m = update_parts(u.n, u.m / 32, n_matrices);
+    u.parts_n = update_parts(u.n, u.n / 32, n_matrices);
+    const int64_t parts = u.parts_m > u.parts_n ? u.parts_m : u.parts_n, t = (u.n + 127) / 128;
+    u.bytes = u.sums_at + (parts > 1 ? parts * n_matrices * (t * (t + 1) / 2) * 128 * 128 * 4 : 0);
     return u;
 }
 
@@ -348,22 +599,43 @@ int power_for(double most)
     return kMostPower - e;
 }
 
+constexpr int64_t kFewTiles = 100;                  // of 64 x 64: up to there tiles of 32 x 32 wait less than they read more
+
 template <Product KIND, typename T>
 hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
 {
     constexpr bool kSymmetric = KIND == GRAM || KIND == POLY;
-    auto tiles = [&](int64_t t) {
-        g.tiles_r = (g.rows + t - 1) / t;
-        g.tiles_c = (g.cols + t - 1) / t;
-        return (kSymmetric ? g.tiles_r * (g.tiles_r + 1) / 2 : g.tiles_r * g.tiles_c);
+    auto tiles = [&](int64_t r, int64_t c) {
+        g.tiles_r = (g.rows + r - 1) / r;
+        g.tiles_c = (g.cols + c - 1) / c;
+        return (kSymmetric ? g.tiles_r * (g.tiles_r + 1) / 2 : g.tiles_r * g.tiles_c) * n_matrices;
     };
-    const int64_t large = tiles(128);
-    if (large * n_matrices >= 256) {
-        update_product_kernel<KIND, T, 128, 2><<<dim3((uint32_t)(kSymmetric ? large : tile_blocks(large, 1)), (uint32_t)n_matrices), kBlock, 0, st>>>(g);
-    } else {
-        const int64_t small = tiles(64);
-        update_product_kernel<KIND, T, 64, 4><<<dim3((uint32_t)(kSymmetric ? small : tile_blocks(small, 1)), (uint32_t)n_matrices), kBlock, 0, st>>>(g);
+    auto grid = [&] {
+        return dim3((uint32_t)(kSymmetric ? (squares_of(g.tiles_r) * kSquare * kSquare * g.parts + 7) / 8 * 8 : tile_blocks(g.tiles_r * g.tiles_c, 1)),
+                    (uint32_t)n_matrices);
+    };
+    if (tiles(64, 64) <= kFewTiles) {
+        tiles(kSmallTile, kSmallTile);
+        const int64_t blocks = kSymmetric ? g.tiles_r * (g.tiles_r + 1) / 2 : g.tiles_r * g.tiles_c;
+        update_small_product_kernel<KIND, T><<<dim3((uint32_t)blocks, (uint32_t)n_matrices), kSmallWaves * kWave, 0, st>>>(g);
+        return hipGetLastError();
     }
+    if constexpr (kSymmetric) {
+        if (g.parts > 1 || tiles(128, 128) >= 256) {
+            tiles(128, 128);
+            update_product_kernel<KIND, T, 128, 128, 2><<<grid(), kBlock, 0, st>>>(g);
+            if (g.parts > 1) {
+                if (hipError_t e = hipGetLastError()) return e;
+                update_join_kernel<KIND, 128><<<dim3((uint32_t)(g.tiles_r * (g.tiles_r + 1) / 2), (uint32_t)n_matrices, 4), kBlock, 0, st>>>(g);
+            }
+            return hipGetLastError();
+        }
+    } else if (tiles(256, 128) >= 200) {
+        update_product_kernel<KIND, T, 256, 128, 3><<<grid(), kBlock, 0, st>>>(g);
+        return hipGetLastError();
+    }
+    tiles(64, 64);
+    update_product_kernel<KIND, T, 64, 64, 4><<<grid(), kBlock, 0, st>>>(g);
     return hipGetLastError();
 }
 
@@ -405,12 +677,15 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
         gram.pitch_same = gram.pitch_other = pitch_n;
         gram.bytes_p = gram.bytes_q = u.big;
         gram.bytes_d = u.small;
+        gram.parts = u.parts_m;
+        gram.sums = (float *)(work + u.sums_at);
         gram.scale = ldexpf(1.0f, a_power[s] - 2 * x_power[s]);
         if (hipError_t e = launch_product<GRAM, float>(gram, n_matrices, st)) return e;
         ProductArgs poly = gram;
         poly.p = poly.q = a;
         poly.lines = lines_n;
         poly.pitch = pitch_n;
+        poly.parts = u.parts_n;
         poly.same = poly.other = q;
         poly.bytes_p = poly.bytes_q = u.small;
         poly.scale = ldexpf(abc[2], q_power[s] - 2 * a_power[s]);
@@ -418,6 +693,7 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
         poly.diagonal = ldexpf(abc[0], q_power[s]);
         if (hipError_t e = launch_product<POLY, float>(poly, n_matrices, st)) return e;
         ProductArgs step{};
+        step.parts = 1;
         step.lines = lines_n;
         step.pitch = pitch_n;
         if (s + 1 < n_steps) {                      // X^T Q, stored both ways
