@@ -216,9 +216,12 @@ def _dev(t: Optional[torch.Tensor], dtype: torch.dtype, name: str) -> Optional[i
     return t.data_ptr()
 
 
+# The current stream's handle without a Stream object around it: 0.4 instead of 2.9 us of a small call's 10 (torch's own compiled code takes it the same way).
+_current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream(stream: Optional[torch.cuda.Stream]) -> Optional[int]:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream or None
+    return (_current_raw_stream(torch.cuda.current_device()) if stream is None else stream.cuda_stream) or None
 
 
 def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
@@ -920,12 +923,13 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 def _elements(t: torch.Tensor, dim: int, name: str) -> Tuple[int, int, int, int]:
     """(pointer, rows, leading dimension, type) of a 2-D fp32 or bf16 device tensor whose rows are contiguous and hold `dim` columns."""
-    if not t.is_cuda or t.dtype not in _TYPES or t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    shape, stride, kind = t.shape, t.stride(), _TYPES.get(t.dtype)
+    if not t.is_cuda or kind is None or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise TypeError(f"{name} must be a 2-D fp32 or bf16 device tensor with unit column stride")
-    if t.shape[1] < dim:
-        raise ValueError(f"{name} has {t.shape[1]} columns, {dim} are wanted")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    return t.data_ptr(), t.shape[0], ld, _TYPES[t.dtype]
+    rows, cols = shape
+    if cols < dim:
+        raise ValueError(f"{name} has {cols} columns, {dim} are wanted")
+    return t.data_ptr(), rows, stride[0] if rows > 1 else max(stride[0], cols), kind
 
 
 def _vector(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
@@ -939,9 +943,10 @@ def _workspace(t: Optional[torch.Tensor]) -> Tuple[Optional[int], int]:
     return _dev(t, torch.uint8, "workspace"), 0 if t is None else t.numel()
 
 
-def _same(name: str, *values) -> None:
-    if len(set(values)) > 1:
-        raise ValueError(f"{name}: the tensors differ in rows or type")
+def _same(name: str, first, *others) -> None:
+    for other in others:
+        if other != first:
+            raise ValueError(f"{name}: the tensors differ in rows or type")
 
 
 def _count(name: str, *args) -> int:

@@ -11,7 +11,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libadaqp.so")
 SOURCES = ["codec.hip", "spmm.hip", "spmm_sliced.hip", "spmm_pieces.hip", "layer.hip", "assign.hip", "spmm_tiled.hip", "spmm_panels.hip",
-           "spmm_blocks.hip", "probe.hip", "norm.hip", "mx4.hip", "mx4_matmul.hip", "orthogonalize.hip"]
+           "spmm_blocks.hip", "probe.hip", "norm.hip", "mx4.hip", "mx4_matmul.hip", "orthogonalize.hip",
+           "orthogonalize_small.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # -ffp-contract=off: the integer codes depend on every fp32 rounding, so nothing may be fused behind our back.

@@ -10,16 +10,11 @@
 // runs along rows of both operands.
 #include <math.h>
 
-#include "elements.hpp"
 #include "lines.hpp"
+#include "orthogonalize.hpp"
 
 namespace adaqp {
 namespace {
-
-typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-typedef _Float16 half4 __attribute__((ext_vector_type(4)));
-typedef _Float16 half2 __attribute__((ext_vector_type(2)));
-typedef float sums16 __attribute__((ext_vector_type(16)));
 
 constexpr int kPad = 64;                            // rows and columns of the held matrices are multiples
 constexpr int kNormBlocks = 512;                    // of a matrix, at most
@@ -29,21 +24,6 @@ constexpr int64_t kMostSize = (int64_t)1 << 20;
 
 // Where (row, col) of a held matrix lies: hi there, lo 64 bytes on.
 __device__ __forceinline__ int64_t held_at(int64_t row, int64_t col, int64_t pitch) { return row * pitch + col / 32 * kLine + col % 32 * 2; }
-
-__device__ __forceinline__ void split(float v, _Float16 &hi, _Float16 &lo)
-{
-    hi = (_Float16)v;
-    lo = (_Float16)(v - (float)hi);
-}
-
-__device__ __forceinline__ double block_sum(double v, double *lds)
-{
-    for (int other = 1; other < kWave; other *= 2) v += __shfl_xor(v, other);
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) lds[threadIdx.x / kWave] = v;
-    __syncthreads();
-    return (lds[0] + lds[1]) + (lds[2] + lds[3]);
-}
 
 // Sums of squares of a share of each matrix: blocks [x] of matrix [y], runs of eight columns a thread.
 template <typename T>
@@ -647,6 +627,17 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
     double *partial = (double *)(work + u.partial_at);
     const int64_t line = 128 / sizeof(T);
     const int64_t written = whole_lines(out, ldo, sizeof(T)) && stride_o * (int64_t)sizeof(T) % 128 == 0 ? (n_cols + line - 1) / line * line : n_cols;
+    if (n_steps > 0 && small_update_fits(n_rows, n_cols)) {
+        SmallUpdate small{g, out, ldg, stride_g, ldo, stride_o, (int32_t)n_rows, (int32_t)n_cols, (int32_t)written, n_steps, eps, x_power[0]};
+        for (int32_t s = 0; s < n_steps; ++s) {
+            small.of_gram[s] = ldexpf(1.0f, a_power[s] - 2 * x_power[s]);
+            small.of_poly[s] = ldexpf(coef[3 * s + 2], q_power[s] - 2 * a_power[s]);
+            small.linear[s] = ldexpf(coef[3 * s + 1], q_power[s] - a_power[s]);
+            small.diagonal[s] = ldexpf(coef[3 * s], q_power[s]);
+            small.of_step[s] = ldexpf(1.0f, (s + 1 < n_steps ? x_power[s + 1] : 0) - x_power[s] - q_power[s]);
+        }
+        return launch_small_update(small, n_matrices, sizeof(T) == 4 ? ADAQP_F32 : ADAQP_BF16, st);
+    }
     update_norm_kernel<T><<<dim3((uint32_t)u.norm_blocks, (uint32_t)n_matrices), kBlock, 0, st>>>(g, ldg, stride_g, n_rows, n_cols, partial);
     if (hipError_t e = hipGetLastError()) return e;
     if (n_steps == 0) {
@@ -734,8 +725,6 @@ int check_sizes(int32_t n_matrices, int64_t n_rows, int64_t n_cols)
     if (n_matrices < 0 || n_rows < 0 || n_cols < 0) return ADAQP_EINVAL;
     return n_matrices > 65535 || n_rows >= kMostSize || n_cols >= kMostSize ? ADAQP_ESIZE : ADAQP_OK;
 }
-
-constexpr int kMostSteps = 64;
 
 }  // namespace
 }  // namespace adaqp
