@@ -17,6 +17,18 @@ __device__ __forceinline__ void load_elements(const T *p, float (&dst)[N])
     for (int k = 0; k < N; ++k) dst[k] = (float)v[k];
 }
 
+// The same, aligned to one element only: one access all the same, the memory system takes any alignment.
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) loose_of { vec_of<T, N> v; };
+
+template <typename T, int N>
+__device__ __forceinline__ void load_loose(const T *p, float (&dst)[N])
+{
+    const vec_of<T, N> v = reinterpret_cast<const loose_of<T, N> *>(p)->v;
+#pragma unroll
+    for (int k = 0; k < N; ++k) dst[k] = (float)v[k];
+}
+
 template <typename T, int N>
 __device__ __forceinline__ vec_of<T, N> rounded(const float (&src)[N])
 {
@@ -32,6 +44,12 @@ __device__ __forceinline__ void store_elements(T *p, const float (&src)[N])
     const vec_of<T, N> v = rounded<T, N>(src);
     if constexpr (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<vec_of<T, N> *>(p));
     else                  *reinterpret_cast<vec_of<T, N> *>(p) = v;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_loose(T *p, const float (&src)[N])
+{
+    reinterpret_cast<loose_of<T, N> *>(p)->v = rounded<T, N>(src);
 }
 
 // The sum over the LANES neighbouring lanes that share lane / LANES, in all of them, without the LDS: exchanges inside rows of 16 lanes by DPP,

@@ -35,7 +35,7 @@ __device__ __forceinline__ void arrived()
 // Which 16 bytes of a line this lane loads with the i-th load of a wave: 8 rows each, the first a multiple of 16.
 __device__ __forceinline__ uint32_t part_of_lane(int i) { return threadIdx.x % 8 ^ (i % 2 * 4 + threadIdx.x % kWave / 16); }
 
-// The places of a wave's loads of a tile of ROWS rows, relative to the tile's first row.  Rows behind the matrix's last take that one's place: what is
+// The places of a wave's loads of a tile of ROWS rows, one of four waves' that load it together, relative to the tile's first row.  Rows behind the matrix's last take that one's place: what is
 // computed from them is not stored.  256 rows of a pitch of 2^24 bytes still fit.
 template <int ROWS>
 struct TileLoads {
@@ -45,7 +45,7 @@ struct TileLoads {
 
     __device__ __forceinline__ TileLoads(int64_t row0, int64_t n_rows, int64_t pitch)
     {
-        const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+        const int wave = threadIdx.x % kBlock / kWave, lane = threadIdx.x % kWave;
         const uint32_t last = (uint32_t)min((int64_t)ROWS, n_rows - row0) - 1;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
@@ -57,7 +57,7 @@ struct TileLoads {
     // Where the wave's loads into a buffer go.
     __device__ __forceinline__ static uint32_t place(const uint8_t *lds)
     {
-        return __builtin_amdgcn_readfirstlane(lds_offset(lds) + threadIdx.x / kWave * (ROWS / kWavesPerBlock) * kLine);
+        return __builtin_amdgcn_readfirstlane(lds_offset(lds) + threadIdx.x % kBlock / kWave * (ROWS / kWavesPerBlock) * kLine);
     }
 
     // Load i of one line of each row; `from` is that line of the tile's first row.  With `half` the second half of the lines does not exist, and the first is

@@ -5,6 +5,9 @@
 // within a wave (64 / LPR rows in one), longer ones take the 256 lanes of a workgroup; rows beyond the registers of those are walked in memory.
 // Both directions are bound by memory: 8 and 12 bytes for about 8 and 15 operations on an element of fp32.
 //
+// Rows of bf16 that begin anywhere are read and written in vectors all the same, aligned to two bytes: 40 000 x 1937 forward 170 us with an element a
+// lane.  Their last vector ends with the row and begins inside the one before; what both have counts once in the sums.
+//
 // The gradients of gamma and beta are sums over rows.  A lane keeps the same columns for all its rows, so it adds them up in
 // registers; a workgroup leaves one row of sums, and a second kernel adds those in order.
 #include "elements.hpp"
@@ -12,7 +15,7 @@
 namespace adaqp {
 namespace {
 
-constexpr int kMostBlocks = 1024;       // of the backward pass: each leaves a row of sums
+constexpr int kMostBlocks = 2048;       // of the backward pass: each leaves a row of sums
 
 struct NormArgs {
     const void *x, *dy;
@@ -42,26 +45,76 @@ __device__ __forceinline__ float row_sum(float v, float *lds)
     }
 }
 
-// The vector of columns [col, col + VW), zeros from column dim on.
-template <typename T, int VW>
-__device__ __forceinline__ void load_columns(const T *row, int32_t col, int32_t dim, float (&v)[VW])
+// How rows lie: PLAIN, whole vectors on multiples of their size; LINES, whole 128-byte lines (zeros behind the columns), dim a multiple of the vector;
+// LINES_TAIL, the same with a vector that holds the last columns and padding; LOOSE, aligned to an element, the last vector moved back to end with the row.
+enum Rows { PLAIN, LINES, LINES_TAIL, LOOSE };
+
+// The columns of vector i: from `col` on; of its VW elements those from `first` to before `end` are its own.
+template <Rows MODE, int VW>
+struct Columns {
+    int32_t col;
+    int first, end;
+    __device__ __forceinline__ Columns(int32_t i, int32_t dim) : col(i * VW), first(0), end(VW)
+    {
+        if (MODE == LINES_TAIL) end = min(VW, dim - col);
+        if (MODE == LOOSE) {
+            col = min(col, dim - VW);
+            first = i * VW - col;
+        }
+    }
+    __device__ __forceinline__ float own(int k, float v) const { return (MODE == LINES_TAIL && k >= end) || (MODE == LOOSE && k < first) ? 0.0f : v; }
+
+    // f(whole) with an integral constant: whether all elements are the vector's own.  One lane of a row has a vector where they are not: the others do without the
+    // selections.
+    template <typename F>
+    __device__ __forceinline__ void with(F f) const
+    {
+        if (MODE == PLAIN || MODE == LINES || (first == 0 && end == VW)) f(std::true_type());
+        else                                                             f(std::false_type());
+    }
+};
+
+template <typename T, int VW, Rows MODE>
+__device__ __forceinline__ void load_columns(const T *row, const Columns<MODE, VW> &c, float (&v)[VW])
 {
-    load_elements<T, VW>(row + col, v);
-    if (VW > 1 && col + VW > dim) {
+    if (MODE == LOOSE) load_loose<T, VW>(row + c.col, v);
+    else               load_elements<T, VW>(row + c.col, v);
+    if (MODE == LINES_TAIL && c.end < VW)
+#pragma unroll
+        for (int k = 0; k < VW; ++k) v[k] = c.own(k, v[k]);
+}
+
+template <typename T, int VW, Rows MODE>
+__device__ __forceinline__ void store_columns(T *row, const Columns<MODE, VW> &c, const float (&v)[VW])
+{
+    if constexpr (MODE == LOOSE) store_loose<T, VW>(row + c.col, v);
+    else                         store_elements<T, VW, MODE != PLAIN>(row + c.col, v);
+}
+
+template <Rows MODE, int VW>
+__device__ __forceinline__ void load_params(const float *p, int32_t i, int32_t n_vec, int32_t dim, float other, float (&v)[VW])
+{
+#pragma unroll
+    for (int k = 0; k < VW; ++k) v[k] = other;
+    if (!p || i >= n_vec) return;
+    const Columns<MODE, VW> c(i, dim);
+    if (c.end == VW) {
+        constexpr int W = VW < 4 ? VW : 4;
+#pragma unroll
+        for (int k = 0; k < VW; k += W) {
+            float part[W];
+            load_loose<float, W>(p + c.col + k, part);
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[k + j] = part[j];
+        }
+    } else {
 #pragma unroll
         for (int k = 0; k < VW; ++k)
-            if (col + k >= dim) v[k] = 0.0f;
+            if (k < c.end) v[k] = p[c.col + k];
     }
 }
 
-template <int VW>
-__device__ __forceinline__ void load_params(const float *p, int32_t col, int32_t dim, float other, float (&v)[VW])
-{
-#pragma unroll
-    for (int k = 0; k < VW; ++k) v[k] = p && col + k < dim ? p[col + k] : other;
-}
-
-template <typename T, int VW, int LPR, int NV, bool WHOLE>
+template <typename T, int VW, int LPR, int NV, Rows MODE>
 __global__ __launch_bounds__(kBlock) void layernorm_forward_kernel(NormArgs a)
 {
     constexpr int kRows = kBlock / LPR;
@@ -70,8 +123,8 @@ __global__ __launch_bounds__(kBlock) void layernorm_forward_kernel(NormArgs a)
     float gamma[NV][VW], beta[NV][VW];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_params<VW>(a.gamma, (v * LPR + l) * VW, a.dim, 1.0f, gamma[v]);
-        load_params<VW>(a.beta, (v * LPR + l) * VW, a.dim, 0.0f, beta[v]);
+        load_params<MODE, VW>(a.gamma, v * LPR + l, a.n_vec, a.dim, 1.0f, gamma[v]);
+        load_params<MODE, VW>(a.beta, v * LPR + l, a.n_vec, a.dim, 0.0f, beta[v]);
     }
     const float dim = (float)a.dim;
     for (int64_t row = (int64_t)blockIdx.x * kRows + r; row < a.n_rows; row += (int64_t)gridDim.x * kRows) {
@@ -80,23 +133,38 @@ __global__ __launch_bounds__(kBlock) void layernorm_forward_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int32_t i = v * LPR + l;
-            if (i < a.n_vec) load_columns<T, VW>(x, i * VW, a.dim, h[v]);
+            if (i < a.n_vec) load_columns<T, VW, MODE>(x, Columns<MODE, VW>(i, a.dim), h[v]);
             else for (int k = 0; k < VW; ++k) h[v][k] = 0.0f;
         }
         float sum = 0.0f;
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
+            if (MODE == LOOSE) {
+                const Columns<MODE, VW> c(v * LPR + l, a.dim);
+                c.with([&](auto whole) {
 #pragma unroll
-            for (int k = 0; k < VW; ++k) sum += h[v][k];
+                    for (int k = 0; k < VW; ++k) sum += whole ? h[v][k] : c.own(k, h[v][k]);
+                });
+            } else {
+#pragma unroll
+                for (int k = 0; k < VW; ++k) sum += h[v][k];
+            }
+        }
         const float mean = row_sum<LPR>(sum, lds) / dim;
         sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int32_t col = (v * LPR + l) * VW;
+            const int32_t i = v * LPR + l;
+            if (i < a.n_vec) {
+                const Columns<MODE, VW> c(i, a.dim);
+                c.with([&](auto whole) {
 #pragma unroll
-            for (int k = 0; k < VW; ++k) {
-                h[v][k] -= mean;
-                if (col + k < a.dim) sum = fmaf(h[v][k], h[v][k], sum);
+                    for (int k = 0; k < VW; ++k) {
+                        h[v][k] -= mean;
+                        const float d = whole ? h[v][k] : c.own(k, h[v][k]);
+                        sum = fmaf(d, d, sum);
+                    }
+                });
             }
         }
         const float rstd = 1.0f / sqrtf(row_sum<LPR>(sum, lds) / dim + a.eps);
@@ -108,17 +176,25 @@ __global__ __launch_bounds__(kBlock) void layernorm_forward_kernel(NormArgs a)
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int32_t i = v * LPR + l;
-            if (i < a.n_vec_out) {
-                float o[VW];
+            float o[VW];
+            if (i < a.n_vec) {
+                const Columns<MODE, VW> c(i, a.dim);
 #pragma unroll
-                for (int k = 0; k < VW; ++k) o[k] = i * VW + k < a.dim ? fmaf(h[v][k] * rstd, gamma[v][k], beta[v][k]) : 0.0f;
-                store_elements<T, VW, WHOLE>(y + i * VW, o);
+                for (int k = 0; k < VW; ++k) o[k] = fmaf(h[v][k] * rstd, gamma[v][k], beta[v][k]);
+                if (MODE == LINES_TAIL && c.end < VW)
+#pragma unroll
+                    for (int k = 0; k < VW; ++k) o[k] = c.own(k, o[k]);
+                store_columns<T, VW, MODE>(y, c, o);
+            } else if (MODE != LOOSE && i < a.n_vec_out) {
+#pragma unroll
+                for (int k = 0; k < VW; ++k) o[k] = 0.0f;
+                store_elements<T, VW, MODE != PLAIN>(y + i * VW, o);
             }
         }
     }
 }
 
-template <typename T, int VW, int LPR, int NV, bool WHOLE>
+template <typename T, int VW, int LPR, int NV, Rows MODE>
 __global__ __launch_bounds__(kBlock) void layernorm_backward_kernel(NormArgs a)
 {
     constexpr int kRows = kBlock / LPR, kCols = LPR * NV * VW;
@@ -127,7 +203,7 @@ __global__ __launch_bounds__(kBlock) void layernorm_backward_kernel(NormArgs a)
     float gamma[NV][VW], dgamma[NV][VW], dbeta[NV][VW];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        load_params<VW>(a.gamma, (v * LPR + l) * VW, a.dim, 1.0f, gamma[v]);
+        load_params<MODE, VW>(a.gamma, v * LPR + l, a.n_vec, a.dim, 1.0f, gamma[v]);
 #pragma unroll
         for (int k = 0; k < VW; ++k) dgamma[v][k] = dbeta[v][k] = 0.0f;
     }
@@ -139,24 +215,32 @@ __global__ __launch_bounds__(kBlock) void layernorm_backward_kernel(NormArgs a)
         for (int v = 0; v < NV; ++v) {
             const int32_t i = v * LPR + l;
             if (i < a.n_vec) {
-                load_columns<T, VW>(x, i * VW, a.dim, h[v]);
-                load_columns<T, VW>(dy, i * VW, a.dim, g[v]);
-            } else for (int k = 0; k < VW; ++k) h[v][k] = g[v][k] = 0.0f;
+                load_columns<T, VW, MODE>(x, Columns<MODE, VW>(i, a.dim), h[v]);
+                load_columns<T, VW, MODE>(dy, Columns<MODE, VW>(i, a.dim), g[v]);
+            }
         }
         const float mean = a.stats_in[2 * row], rstd = a.stats_in[2 * row + 1];
         float first = 0.0f, second = 0.0f;
 #pragma unroll
-        for (int v = 0; v < NV; ++v)
+        for (int v = 0; v < NV; ++v) {
+            const int32_t i = v * LPR + l;
+            if (i < a.n_vec) {
+                const Columns<MODE, VW> c(i, a.dim);
+                c.with([&](auto whole) {
 #pragma unroll
-            for (int k = 0; k < VW; ++k) {
-                h[v][k] = (h[v][k] - mean) * rstd;            // behind the last column g is 0, and what h is does not matter: unless it is not finite
-                if ((v * LPR + l) * VW + k >= a.dim) h[v][k] = 0.0f;
-                dgamma[v][k] = fmaf(g[v][k], h[v][k], dgamma[v][k]);
-                dbeta[v][k] += g[v][k];
-                g[v][k] *= gamma[v][k];
-                first += g[v][k];
-                second = fmaf(g[v][k], h[v][k], second);
+                    for (int k = 0; k < VW; ++k) {
+                        h[v][k] = (h[v][k] - mean) * rstd;
+                        const float own_h = whole ? h[v][k] : c.own(k, h[v][k]), d = whole ? g[v][k] : c.own(k, g[v][k]);
+                        dgamma[v][k] = fmaf(d, own_h, dgamma[v][k]);
+                        dbeta[v][k] += d;
+                        g[v][k] *= gamma[v][k];
+                        const float own_g = whole ? g[v][k] : c.own(k, g[v][k]);
+                        first += own_g;
+                        second = fmaf(own_g, own_h, second);
+                    }
+                });
             }
+        }
         if (a.out) {
             first = row_sum<LPR>(first, lds) / dim;
             second = row_sum<LPR>(second, lds) / dim;
@@ -164,17 +248,26 @@ __global__ __launch_bounds__(kBlock) void layernorm_backward_kernel(NormArgs a)
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int32_t i = v * LPR + l;
-                if (i < a.n_vec_out) {
-                    float o[VW];
+                float o[VW];
+                if (i < a.n_vec) {
+                    const Columns<MODE, VW> c(i, a.dim);
 #pragma unroll
-                    for (int k = 0; k < VW; ++k) o[k] = i * VW + k < a.dim ? rstd * (g[v][k] - fmaf(h[v][k], second, first)) : 0.0f;
-                    store_elements<T, VW, WHOLE>(dx + i * VW, o);
+                    for (int k = 0; k < VW; ++k) o[k] = rstd * (g[v][k] - fmaf(h[v][k], second, first));
+                    if (MODE == LINES_TAIL && c.end < VW)
+#pragma unroll
+                        for (int k = 0; k < VW; ++k) o[k] = c.own(k, o[k]);
+                    store_columns<T, VW, MODE>(dx, c, o);
+                } else if (MODE != LOOSE && i < a.n_vec_out) {
+#pragma unroll
+                    for (int k = 0; k < VW; ++k) o[k] = 0.0f;
+                    store_elements<T, VW, MODE != PLAIN>(dx + i * VW, o);
                 }
             }
         }
     }
     if (!a.partial) return;
     float *to = a.partial + (int64_t)blockIdx.x * 2 * a.dim;
+    const int32_t last = (a.n_vec - 1) * VW;        // column of the last vector, which a LOOSE one may be behind
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         __syncthreads();
@@ -184,8 +277,9 @@ __global__ __launch_bounds__(kBlock) void layernorm_backward_kernel(NormArgs a)
             for (int k = 0; k < VW; ++k) lds[r * kCols + (v * LPR + l) * VW + k] = which ? dbeta[v][k] : dgamma[v][k];
         __syncthreads();
         for (int32_t col = threadIdx.x; col < a.dim; col += kBlock) {
+            const int32_t at = MODE == LOOSE && col >= last ? col + last + VW - a.dim : col;
             float sum = 0.0f;
-            for (int q = 0; q < kRows; ++q) sum += lds[q * kCols + col];
+            for (int q = 0; q < kRows; ++q) sum += lds[q * kCols + at];
             to[which * a.dim + col] = sum;
         }
     }
@@ -275,21 +369,23 @@ struct NormShape {
 constexpr int kLongLanes = 0;
 
 // Lanes per row: the fewest of 8, 16, 32, 64 that have at most four vectors each, then 64 with up to eight, then a workgroup.
-NormShape norm_shape(int64_t n_rows, int32_t dim, int vw)
+// `cols`: that are read or written.
+NormShape norm_shape(int64_t n_rows, int64_t cols, int vw)
 {
     NormShape s{vw, kLongLanes, 0, 0};
-    const int64_t n_vec = (dim + vw - 1) / vw;
+    const int64_t n_vec = (cols + vw - 1) / vw;
     if (n_vec <= 64 * 8) {
         s.lpr = 8;
         while (s.lpr < 64 && n_vec > s.lpr * 4) s.lpr *= 2;
-        s.nv = n_vec <= s.lpr * 4 ? 4 : n_vec <= s.lpr * 6 ? 6 : 8;
+        s.nv = s.lpr == 64 && n_vec <= 64 * 3 ? 3 : n_vec <= s.lpr * 4 ? 4 : n_vec <= s.lpr * 6 ? 6 : 8;
     } else if (n_vec <= kBlock * 8 && vw * 8 <= 32) {
         s.lpr = kBlock;
         s.nv = n_vec <= kBlock * 4 ? 4 : 8;
     }
     const int64_t rows = s.lpr ? kBlock / s.lpr : 1;
     s.blocks = (n_rows + rows - 1) / rows;
-    if (s.blocks > kMostBlocks) s.blocks = kMostBlocks;
+    const int64_t most = s.nv * s.vw <= 8 ? kMostBlocks : kMostBlocks / 2;
+    if (s.blocks > most) s.blocks = most;
     return s;
 }
 
@@ -303,7 +399,8 @@ void with_shape(const NormShape &s, F f)
     else if (s.lpr == 16) f(W(), integral_constant<int, 16>(), integral_constant<int, 4>());
     else if (s.lpr == 32) f(W(), integral_constant<int, 32>(), integral_constant<int, 4>());
     else if (s.lpr == 64) {
-        if (s.nv == 4)      f(W(), integral_constant<int, 64>(), integral_constant<int, 4>());
+        if (s.nv == 3)      f(W(), integral_constant<int, 64>(), integral_constant<int, 3>());
+        else if (s.nv == 4) f(W(), integral_constant<int, 64>(), integral_constant<int, 4>());
         else if (VW <= 4 && s.nv == 6) f(W(), integral_constant<int, 64>(), integral_constant<int, VW <= 4 ? 6 : 4>());
         else if (VW <= 4) f(W(), integral_constant<int, 64>(), integral_constant<int, VW <= 4 ? 8 : 4>());
     } else if (VW <= 4) {
@@ -315,29 +412,38 @@ void with_shape(const NormShape &s, F f)
 template <typename T>
 constexpr int most_elements() { return 16 / (int)sizeof(T); }
 
-// Vectors for all matrices of a call, and whether rows are written in whole lines.
-struct NormLayout { int vw; bool whole; };
-
-NormLayout norm_layout(const void *x, int64_t ldx, const void *dy, int64_t lddy, const void *out, int64_t ldo, int32_t dim, int64_t bytes)
-{
-    NormLayout n;
-    n.whole = out && whole_lines(out, ldo, bytes);
-    const bool all = whole_lines(x, ldx, bytes) && (!dy || whole_lines(dy, lddy, bytes)) && (!out || n.whole);
-    if (all) n.vw = (int)(16 / bytes);                      // rows own their lines: the last vector may reach into the padding
-    else {
-        n.vw = vector_elements(x, ldx, dim, bytes);
-        if (dy) { const int w = vector_elements(dy, lddy, dim, bytes); if (w < n.vw) n.vw = w; }
-        if (out) { const int w = vector_elements(out, ldo, dim, bytes); if (w < n.vw) n.vw = w; }
-    }
-    // 8 elements in a lane's vector: with more than four such the registers of two vectors of sums do not suffice
-    if (n.vw == 8 && (dim + 7) / 8 > 64 * 4) n.vw = 4;
-    return n;
-}
-
 int32_t columns_written(bool whole, int32_t dim, int64_t bytes)
 {
     const int32_t line = (int32_t)(128 / bytes);
     return whole ? (dim + line - 1) / line * line : dim;
+}
+
+// Vectors for all matrices of a call, how rows lie, and whether those that are written have whole lines.
+struct NormLayout { int vw; Rows mode; bool whole; };
+
+NormLayout norm_layout(const void *x, int64_t ldx, const void *dy, int64_t lddy, const void *out, int64_t ldo, int32_t dim, int64_t bytes)
+{
+    NormLayout n;
+    // Vectors of 8 bf16 up to 2048 columns, beyond which the registers do not suffice; backward, which keeps five numbers a column, 4 up to 1024 (us with 8 and 4:
+    // 58 000 x 602 87, 61; 24 000 x 301 21, 18; 40 000 x 1937 118, 166; forward 306 000 x 256 66, 99).
+    const int most = (int)(16 / bytes), wide = dim > 2048 || (dy && dim <= 1024) ? 4 : 8;
+    n.whole = out && whole_lines(out, ldo, bytes);
+    n.mode = PLAIN;
+    const bool all = whole_lines(x, ldx, bytes) && (!dy || whole_lines(dy, lddy, bytes)) && (!out || n.whole);
+    if (all) {
+        n.vw = most < wide ? most : wide;                   // rows own their lines: the last vector may reach into the padding
+        n.mode = dim % n.vw ? LINES_TAIL : LINES;
+        return n;
+    }
+    n.vw = vector_elements(x, ldx, dim, bytes);
+    if (dy) { const int w = vector_elements(dy, lddy, dim, bytes); if (w < n.vw) n.vw = w; }
+    if (out) { const int w = vector_elements(out, ldo, dim, bytes); if (w < n.vw) n.vw = w; }
+    if (n.vw > wide) n.vw = wide;
+    if (bytes == 2 && n.vw <= 2 && dim >= 8 && !n.whole) {
+        n.vw = wide;
+        n.mode = LOOSE;
+    }
+    return n;
 }
 
 template <typename T, bool BACKWARD>
@@ -357,12 +463,18 @@ hipError_t launch_norm(NormArgs a, const NormLayout &n, const NormShape &s, hipS
         const int64_t rows = kBlock / LPR;
         int64_t blocks = BACKWARD ? s.blocks : (a.n_rows + rows - 1) / rows;
         if (blocks > 2048) blocks = 2048;
-        if constexpr (BACKWARD) {
-            if (n.whole) layernorm_backward_kernel<T, VW, LPR, NV, true><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
-            else         layernorm_backward_kernel<T, VW, LPR, NV, false><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
-        } else {
-            if (n.whole) layernorm_forward_kernel<T, VW, LPR, NV, true><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
-            else         layernorm_forward_kernel<T, VW, LPR, NV, false><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
+        auto run = [&](auto mode) {
+            constexpr Rows MODE = decltype(mode)::value;
+            if constexpr (BACKWARD) layernorm_backward_kernel<T, VW, LPR, NV, MODE><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
+            else                    layernorm_forward_kernel<T, VW, LPR, NV, MODE><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
+        };
+        constexpr bool kWide = VW * (int)sizeof(T) == 16 || (VW == 4 && sizeof(T) == 2);
+        if (n.mode == PLAIN) run(std::integral_constant<Rows, PLAIN>());
+        if constexpr (kWide) {
+            if (n.mode == LINES) run(std::integral_constant<Rows, LINES>());
+            if (n.mode == LINES_TAIL) run(std::integral_constant<Rows, LINES_TAIL>());
+            if constexpr (sizeof(T) == 2)
+                if (n.mode == LOOSE) run(std::integral_constant<Rows, LOOSE>());
         }
     };
     if (s.vw == 1)      with_shape<T, 1>(s, go);
@@ -396,7 +508,7 @@ extern "C" int adaqp_layernorm_forward(const void *x_dev, int64_t ldx, int64_t n
     a.x = x_dev; a.out = y_dev; a.gamma = gamma_dev; a.beta = beta_dev; a.stats = stats_dev;
     a.n_rows = n_rows; a.ldx = ldx; a.ldo = ldy; a.dim = dim; a.eps = eps;
     const NormLayout n = norm_layout(x_dev, ldx, nullptr, 0, y_dev, ldy, dim, element_bytes(type));
-    const NormShape s = norm_shape(n_rows, dim, n.vw);
+    const NormShape s = norm_shape(n_rows, columns_written(n.whole, dim, element_bytes(type)), n.vw);
     if (type == ADAQP_F32) ADAQP_HIP_TRY((launch_norm<float, false>(a, n, s, (hipStream_t)stream)));
     else                   ADAQP_HIP_TRY((launch_norm<__bf16, false>(a, n, s, (hipStream_t)stream)));
     return ADAQP_OK;
@@ -436,7 +548,7 @@ extern "C" int adaqp_layernorm_backward(const void *x_dev, int64_t ldx, const vo
         a.partial = dgamma_dev ? (float *)workspace_dev : nullptr;
         a.n_rows = n_rows; a.ldx = ldx; a.lddy = lddy; a.ldo = lddx; a.dim = dim;
         const NormLayout n = norm_layout(x_dev, ldx, dy_dev, lddy, dx_dev, lddx, dim, element_bytes(type));
-        s = norm_shape(n_rows, dim, n.vw);
+        s = norm_shape(n_rows, columns_written(n.whole, dim, element_bytes(type)), n.vw);
         if (type == ADAQP_F32) ADAQP_HIP_TRY((launch_norm<float, true>(a, n, s, (hipStream_t)stream)));
         else                   ADAQP_HIP_TRY((launch_norm<__bf16, true>(a, n, s, (hipStream_t)stream)));
     }

@@ -330,22 +330,25 @@ __device__ __forceinline__ void store_sums(const ProductArgs &g, const uint8_t *
     }
 }
 
-// Tiles of TR x TC, a quarter each wave.
-template <Product KIND, typename T, int TR, int TC, int STAGES>
-__global__ __launch_bounds__(kBlock) void update_product_kernel(ProductArgs g)
+// Tiles of TR x TC, a quarter each wave of four.  With GROUPS = 2 eight waves share a tile, every second line each four of them: where there is a tile for each
+// CU at most, half as many lines and barriers come one after the other.
+template <Product KIND, typename T, int TR, int TC, int STAGES, int GROUPS>
+__global__ __launch_bounds__(kBlock * GROUPS) void update_product_kernel(ProductArgs g)
 {
     constexpr bool kSymmetric = KIND == GRAM || KIND == POLY;
     constexpr int FR = TR / 64, FC = TC / 64;       // 32 x 32 parts of a wave
     struct Stage { uint8_t p[TR * kLine], q[TC * kLine]; };
-    __shared__ __align__(16) uint8_t lds[sizeof(Stage) * STAGES];
-    static_assert(sizeof(lds) >= kWavesPerBlock * sizeof(Sheet), "the sheets lie where the operands were");
-    Stage *stage = reinterpret_cast<Stage *>(lds);
+    __shared__ __align__(16) uint8_t lds[sizeof(Stage) * STAGES * GROUPS];
+    static_assert(sizeof(Stage) * STAGES >= kWavesPerBlock * sizeof(Sheet), "the sheets lie where the operands were");
+    static_assert(GROUPS == 1 || sizeof(Stage) * STAGES >= TR * TC * 4, "the other groups' sums, too");
+    const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / kBlock);
+    Stage *stage = reinterpret_cast<Stage *>(lds) + group * STAGES;
     int64_t tr, tc;
     int part;
     if (!product_tile<kSymmetric>(g, tr, tc, part)) return;
     const uint8_t *p = g.p + blockIdx.y * g.bytes_p, *q = g.q + blockIdx.y * g.bytes_q;
     const int64_t row0 = tr * TR, col0 = tc * TC, pitch = g.pitch;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+    const int wave = threadIdx.x % kBlock / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
     const int wr = wave / 2 * (TR / 2), wc = wave % 2 * (TC / 2);
 
     sums16 sums[FR][FC];
@@ -359,12 +362,13 @@ __global__ __launch_bounds__(kBlock) void update_product_kernel(ProductArgs g)
     const TileLoads<TR> of_p(row0, g.rows, pitch);
     const TileLoads<TC> of_q(col0, g.cols, pitch);
     constexpr int kLoadsP = TileLoads<TR>::kLoads, kLoads = kLoadsP + TileLoads<TC>::kLoads;
-    const int per_part = (int)((g.lines + g.parts - 1) / g.parts), begin = part * per_part, lines = min(per_part, (int)g.lines - begin);
-    const uint8_t *from_p = p + row0 * pitch + (int64_t)begin * kLine, *from_q = q + col0 * pitch + (int64_t)begin * kLine;
+    // of the tile, or of the group: sizes are multiples of 64, so there is an even number
+    const int per_part = (int)((g.lines + g.parts - 1) / g.parts), begin = part * per_part, lines = min(per_part, (int)g.lines - begin) / GROUPS;
+    const uint8_t *from_p = p + row0 * pitch + (int64_t)(begin + group) * kLine, *from_q = q + col0 * pitch + (int64_t)(begin + group) * kLine;
     // Load i of a line of both operands.
     auto load = [&](int i, int line, const auto &s) {
-        if (i < kLoadsP) of_p.template load<false>(i, from_p + (int64_t)line * kLine, TileLoads<TR>::place(s.p));
-        else             of_q.template load<false>(i - kLoadsP, from_q + (int64_t)line * kLine, TileLoads<TC>::place(s.q));
+        if (i < kLoadsP) of_p.template load<false>(i, from_p + (int64_t)line * (kLine * GROUPS), TileLoads<TR>::place(s.p));
+        else             of_q.template load<false>(i - kLoadsP, from_q + (int64_t)line * (kLine * GROUPS), TileLoads<TC>::place(s.q));
     };
     // The operands of half a line, 16 columns: read from the LDS while the half before is multiplied.
     struct Half { half8 ph[FR], pl[FR], qh[FC], ql[FC]; } half[2];
@@ -449,6 +453,23 @@ __global__ __launch_bounds__(kBlock) void update_product_kernel(ProductArgs g)
         return;
     }
     arrived<0>();                                   // nobody reads the operands any more
+    if constexpr (GROUPS > 1) {
+        float4 *others = reinterpret_cast<float4 *>(lds + sizeof(Stage) * STAGES);
+        static_assert(GROUPS == 2 && FR == 1 && FC == 1, "one other group's 32 x 32 sums a wave");
+        if (group > 0)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) others[e / 4 * kBlock + threadIdx.x % kBlock] = make_float4(sums[0][0][e], sums[0][0][e + 1], sums[0][0][e + 2], sums[0][0][e + 3]);
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+            const float4 v = others[e / 4 * kBlock + threadIdx.x];
+            sums[0][0][e] += v.x;
+            sums[0][0][e + 1] += v.y;
+            sums[0][0][e + 2] += v.z;
+            sums[0][0][e + 3] += v.w;
+        }
+    }
     Sheet &sheet = reinterpret_cast<Sheet *>(lds)[wave];
 #pragma unroll
     for (int i = 0; i < FR; ++i)
@@ -515,7 +536,7 @@ struct UpdateLayout {
 
 // Cuts of the lines of a symmetric product of n x n: two tiles of 128 x 128 share a CU, and with at least kCutTiles of them there are enough for tiles of that size to
 // pay, but fewer than there is room for.
-constexpr int kCutTiles = 100, kRoom = 512, kLeastLines = 16;
+constexpr int kCutTiles = 128, kRoom = 512, kLeastLines = 16;
 
 int update_parts(int64_t n, int64_t lines, int64_t n_matrices)
 {
@@ -579,7 +600,7 @@ int power_for(double most)
     return kMostPower - e;
 }
 
-constexpr int64_t kFewTiles = 100;                  // of 64 x 64: up to there tiles of 32 x 32 wait less than they read more
+constexpr int64_t kFewTiles = 64;                  // of 64 x 64: up to there tiles of 32 x 32 wait less than they read more
 
 template <Product KIND, typename T>
 hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
@@ -603,19 +624,25 @@ hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
     if constexpr (kSymmetric) {
         if (g.parts > 1 || tiles(128, 128) >= 256) {
             tiles(128, 128);
-            update_product_kernel<KIND, T, 128, 128, 2><<<grid(), kBlock, 0, st>>>(g);
+            update_product_kernel<KIND, T, 128, 128, 2, 1><<<grid(), kBlock, 0, st>>>(g);
             if (g.parts > 1) {
                 if (hipError_t e = hipGetLastError()) return e;
                 update_join_kernel<KIND, 128><<<dim3((uint32_t)(g.tiles_r * (g.tiles_r + 1) / 2), (uint32_t)n_matrices, 4), kBlock, 0, st>>>(g);
             }
             return hipGetLastError();
         }
-    } else if (tiles(256, 128) >= 200) {
-        update_product_kernel<KIND, T, 256, 128, 3><<<grid(), kBlock, 0, st>>>(g);
-        return hipGetLastError();
+    } else {
+        if (tiles(256, 128) >= 256) {
+            update_product_kernel<KIND, T, 256, 128, 3, 1><<<grid(), kBlock, 0, st>>>(g);
+            return hipGetLastError();
+        }
+        if (tiles(128, 128) >= 200) {
+            update_product_kernel<KIND, T, 128, 128, 2, 1><<<grid(), kBlock, 0, st>>>(g);
+            return hipGetLastError();
+        }
     }
-    tiles(64, 64);
-    update_product_kernel<KIND, T, 64, 64, 4><<<grid(), kBlock, 0, st>>>(g);
+    if (tiles(64, 64) <= 256) update_product_kernel<KIND, T, 64, 64, 4, 2><<<grid(), kBlock * 2, 0, st>>>(g);
+    else                      update_product_kernel<KIND, T, 64, 64, 4, 1><<<grid(), kBlock, 0, st>>>(g);
     return hipGetLastError();
 }
 

@@ -158,6 +158,45 @@ def test_layernorm_backward(rows, dim, ld, offset, kind):
     assert torch.equal(dyd, dx)
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("dim", [1, 20, 31, 33, 64, 100, 300, 602, 1000, 2100])
+def test_layernorm_of_matrices_that_lie_differently(dim, kind):
+    """One with whole lines, one that begins anywhere: the definition's values (tolerances as above), and padding only where it is."""
+    _say("layernorm mixed", dim, kind)
+    dtype, rows = TYPES[kind], 37
+    x, gamma, beta, dy = _norm_values(rows, dim, dim)
+    padded = -(-dim // 64) * 64
+    gd, bd = _vec(gamma), _vec(beta)
+    x, dy = _np(_matrix(x, dtype)), _np(_matrix(dy, dtype))
+    y64, mean, rstd = D.layernorm(x, _np(gd), _np(bd), np.float32(1e-5))
+    stats = torch.from_numpy(np.stack([mean, rstd], 1)).float().to(DEV)
+    k = dim / 64 + 48
+    off_mean = k * U * np.abs(x).mean(1)
+    h = (x - mean[:, None]) * rstd[:, None]
+    rel = (k + 8) * U + 0.5 * (off_mean * rstd) ** 2
+    tol_y = np.abs(_np(gd)) * ((off_mean * rstd)[:, None] * (1 + rel[:, None]) + np.abs(h) * rel[:, None]) + 4 * U * (np.abs(h * _np(gd)) + np.abs(_np(bd)))
+    mean, rstd = _np(stats).T
+    dx64, dgamma64, dbeta64 = D.layernorm_backward(x, dy, mean, rstd, _np(gd))
+    h, g = (x - mean[:, None]) * rstd[:, None], dy * _np(gd)
+    k = dim / 64 + 56
+    tol_dx = rstd[:, None] * U * (8 * np.abs(g) + k * np.abs(g).mean(1)[:, None] + (k + 8) * np.abs(h) * np.abs(g * h).mean(1)[:, None])
+    many = rows / 64 + 64
+    work = _bytes(B.adaqp_layernorm_workspace_bytes(rows, dim))
+    for ld_in, at_in, ld_out, at_out in ((padded, 0, dim, 0), (dim + 3, 1, padded, 0), (dim, 0, padded, 0), (padded, 0, dim + 1, 1)):
+        xd = _matrix(x, dtype, ld_in, at_in)
+        y, buf = _out(rows, dim, dtype, ld_out, at_out)
+        B.adaqp_layernorm_forward(xd, dim, gd, bd, 1e-5, y)
+        assert np.all(np.abs(_np(y) - y64) <= tol_y + _rounding(np.abs(y64) + tol_y, dtype) + 1e-38)
+        _untouched(buf, y, rows, dim, ld_out, at_out, dtype)
+        dx, buf = _out(rows, dim, dtype, ld_out, at_out)
+        dgamma, dbeta = torch.empty(dim, device=DEV), torch.empty(dim, device=DEV)
+        B.adaqp_layernorm_backward(xd, _matrix(dy, dtype), dim, stats, gd, dx, dgamma, dbeta, work)
+        assert np.all(np.abs(_np(dx) - dx64) <= tol_dx + _rounding(np.abs(dx64) + tol_dx, dtype) + 1e-38)
+        assert np.all(np.abs(_np(dgamma) - dgamma64) <= (many + 4) * U * np.abs(dy * h).sum(0) + 1e-38)
+        assert np.all(np.abs(_np(dbeta) - dbeta64) <= many * U * np.abs(dy).sum(0) + 1e-38)
+        _untouched(buf, dx, rows, dim, ld_out, at_out, dtype)
+
+
 def test_layernorm_without_parameters_and_rows():
     x = _matrix(np.random.default_rng(0).standard_normal((4, 32)), torch.float32)
     y, plain = torch.empty_like(x), torch.empty_like(x)
@@ -296,6 +335,26 @@ def test_mx4_matmul(m, n, k, kind):
     assert torch.equal(again, out)
 
 
+@pytest.mark.parametrize("m,n,k", [(4200, 2040, 1600), (8200, 4090, 3200), (256, 602, 9000), (100, 90, 20_000), (30, 20, 70_000), (600, 30_000, 700)])
+def test_mx4_matmul_of_every_tile(m, n, k):
+    """The sizes that the larger tiles and the cut sums are for; products by torch in float64 of the values."""
+    _say("mx4 matmul tiles", m, n, k)
+    gen = torch.Generator(device=DEV).manual_seed(m)
+    packed, values = [], []
+    for rows in (m, n):
+        codes, scales = B.mx4_empty(rows, k, DEV)
+        packed.append((codes.random_(0, 256, generator=gen), scales.random_(125, 130, generator=gen)))
+        if k % 128:
+            codes[:, k // 2 + k % 2:].zero_()
+            if k % 2:
+                codes[:, k // 2] &= 15
+        values.append(torch.from_numpy(D.mx4_values(codes.cpu().numpy(), scales.cpu().numpy(), k)).to(DEV))
+    out = torch.empty(m, n, device=DEV)
+    B.adaqp_mx4_matmul(*packed, k, out, _bytes(B.adaqp_mx4_matmul_workspace_bytes(m, n, k)).fill_(0xFF))
+    want, size = values[0] @ values[1].t(), values[0].abs() @ values[1].abs().t()
+    assert bool(((out.double() - want).abs() <= 2 * U * (k / 64 + 16) * size).all())
+
+
 def test_mx4_matmul_of_extreme_scales_nan_blocks_and_nothing():
     (ac, asc), av = _mx_random(40, 200, 1)
     (bc, bsc), bv = _mx_random(50, 200, 2)
@@ -343,7 +402,8 @@ def test_mx4_gradients_of_a_product_are_differences():
 # ---- orthogonalised updates ------------------------------------------------------------------------------------------------------------------------------
 
 UPDATES = [(1, 1, 1), (1, 1, 7), (1, 7, 1), (2, 16, 16), (3, 41, 256), (3, 256, 41), (1, 64, 64), (1, 65, 130), (2, 100, 300), (1, 256, 256), (1, 602, 256),
-           (1, 256, 602), (4, 127, 129), (1, 513, 700), (1, 1100, 1030), (70, 40, 50), (40, 130, 257)]
+           (1, 256, 602), (4, 127, 129), (1, 513, 700), (1, 1100, 1030), (70, 40, 50), (40, 130, 257),
+           (5, 20, 33), (2, 64, 480), (2, 64, 512), (1, 960, 30), (1, 33, 100), (1, 65, 65), (2, 1500, 1400)]
 
 
 def _gradient(count, rows, cols, seed):
