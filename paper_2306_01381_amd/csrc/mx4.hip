@@ -20,6 +20,8 @@ struct MxArgs {
     int64_t ld, n_rows, n_cols;
     uint32_t tiles_r, tiles_c;
     uint32_t row_blocks;                            // blocks of a row that have columns
+    uint32_t row_factor, row_shift;                 // n / row_blocks = n * row_factor >> row_shift for the n below 2^31 that there are; 0: there are more
+    int ragged;                                     // 0: all blocks are full; else the last may end inside a vector (1) or not (2)
     uint64_t seed;
     uint8_t *codes, *scales, *codes_t, *scales_t;
     int64_t pitch, pitch_t;
@@ -47,23 +49,26 @@ __device__ __forceinline__ uint32_t nearest_codes(const float (&x)[8], uint32_t 
     return byte == 255 ? 0 : word;
 }
 
-// A value from 1 on is an fp32 number whose exponent and first fraction bit, counted from those of 1/2, are its code, and whose other 22 fraction bits are
-// the share of the way to the next one; below 2 the code counts steps of 1/2, and the share is in 16 fraction bits of the value times 2^17.
+// Scaled so that 1 is the smallest normal fp32 number, a block's values have the code's own form: below 1 subnormal numbers, from there on exponent and first
+// fraction bit.  Bits 22..24 are the code below the value, the 22 bits behind them the share of the way to the next, and adding the random number to
+// the upper 16 of those carries into the code as often as it should.  What is shifted out of a subnormal number has to be cut off: round_toward_zero().
 __device__ __forceinline__ uint32_t stochastic_codes(const float (&x)[8], uint32_t byte, const Rand128 &rnd)
 {
     const uint32_t w[4] = {rnd.w0, rnd.w1, rnd.w2, rnd.w3};
-    const int power = 127 + 17 - (int)byte;
-    uint32_t word = 0;
+    const int power = 127 - 126 - (int)byte;
+    uint32_t codes = 0, signs = 0;
+#pragma unroll
+    for (int j = 7; j >= 0; --j) signs = __builtin_amdgcn_alignbit(signs, __builtin_bit_cast(uint32_t, x[j]), 28);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const uint32_t r = j % 2 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
-        const float z = __builtin_amdgcn_ldexpf(fabsf(x[j]), power);
-        const uint32_t low = ((uint32_t)z + r) >> 16, high = ((__builtin_bit_cast(uint32_t, z) + (r << 6)) >> 22) - ((127 + 17) * 2 - 2);
-        const uint32_t code = z < 131072.0f ? low : high;
-        word |= (code | (__builtin_bit_cast(uint32_t, x[j]) >> 28 & 8u)) << (4 * j);
+        codes |= ((__builtin_bit_cast(uint32_t, __builtin_amdgcn_ldexpf(fabsf(x[j]), power)) + (r << 6)) >> 22) << (4 * j);
     }
-    return byte == 255 ? 0 : word;
+    return byte == 255 ? 0 : (codes & 0x77777777u) | (signs & 0x88888888u);
 }
+
+// For the wave that calls it and all its fp32 arithmetic from there on: bits 0 and 1 of the mode register.
+__device__ __forceinline__ void round_toward_zero() { __builtin_amdgcn_s_setreg(1 | 0 << 6 | (2 - 1) << 11, 3); }
 
 __device__ __forceinline__ Rand128 random_words(uint64_t seed, int64_t row, int64_t granule)
 {
@@ -105,11 +110,13 @@ __device__ __forceinline__ void load_granule(const MxArgs &a, int64_t row, int64
     }
 }
 
+// STEP: columns that are there or not together.
+template <int STEP>
 __device__ __forceinline__ void keep_granule(const MxArgs &a, int64_t row, int64_t col, float (&x)[8])
 {
     const int left = row < a.n_rows ? (int)min(a.n_cols - col, (int64_t)8) : 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[k] = k < left ? x[k] : 0.0f;
+    for (int k = 0; k < 8; ++k) x[k] = k / STEP * STEP < left ? x[k] : 0.0f;
 }
 
 // The rows' form alone: blocks of 32 columns, kEach for a lane, row by row.
@@ -117,21 +124,23 @@ template <typename T, int VW, bool STOCHASTIC>
 __global__ __launch_bounds__(kBlock) void mx4_quantize_rows_kernel(MxArgs a)
 {
     constexpr int kEach = 2, kBlocks = kBlock / 4;
-    const uint64_t first = (uint64_t)xcd_neighbour(blockIdx.x, gridDim.x) * (kBlocks * kEach) + threadIdx.x / 4, total = (uint64_t)a.n_rows * a.row_blocks;
+    if (STOCHASTIC) round_toward_zero();            // nothing but the scaling rounds here
+    const uint64_t first = (uint64_t)xcd_neighbour(blockIdx.x, gridDim.x) * (kBlocks * kEach) + threadIdx.x / 4;
     const int l = threadIdx.x % 4;
     int64_t row[kEach];
     uint32_t block[kEach];
     float x[kEach][8];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        const uint64_t at = first + e * kBlocks;
-        row[e] = total >> 32 ? at / a.row_blocks : (uint32_t)at / a.row_blocks;        // at may lie behind the last: so does its row
-        block[e] = (uint32_t)(at - row[e] * a.row_blocks);
+        const uint64_t at = first + e * kBlocks;    // may lie behind the last block: so does its row then
+        row[e] = a.row_factor ? (uint64_t)(uint32_t)at * a.row_factor >> a.row_shift : at / a.row_blocks;
+        block[e] = (uint32_t)at - (uint32_t)row[e] * a.row_blocks;
         load_granule<T, VW>(a, row[e], block[e] * kMxBlock + l * 8, x[e]);
     }
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        keep_granule(a, row[e], block[e] * kMxBlock + l * 8, x[e]);
+        if (a.ragged == 1) keep_granule<1>(a, row[e], block[e] * kMxBlock + l * 8, x[e]);
+        if (a.ragged > 1) keep_granule<VW>(a, row[e], block[e] * kMxBlock + l * 8, x[e]);
         uint32_t most = magnitude(largest<8>(x[e]));
         most = max(most, moved<kSwap1>(most));
         most = max(most, moved<kSwap2>(most));
@@ -155,6 +164,7 @@ __global__ __launch_bounds__(kBlock) void mx4_quantize_kernel(MxArgs a)
 {
     constexpr int kRows = 64, kPasses = kRows / kPassRows;
     __shared__ float tile[kRows * kMxChunk];
+    if (STOCHASTIC) round_toward_zero();
     // an XCD gets neighbouring tiles, four tile rows together: their parts of the columns' lines meet in its L2
     constexpr uint32_t kGroup = 4;
     const uint32_t at = xcd_neighbour(blockIdx.x, gridDim.x);
@@ -172,7 +182,7 @@ __global__ __launch_bounds__(kBlock) void mx4_quantize_kernel(MxArgs a)
     }
     if ((tile_r + 1) * kRows > a.n_rows || (chunk_c + 1) * kMxChunk > a.n_cols)
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) keep_granule(a, tile_r * kRows + p * kPassRows + r, col, x[p]);
+        for (int p = 0; p < kPasses; ++p) keep_granule<1>(a, tile_r * kRows + p * kPassRows + r, col, x[p]);
     {
         // rows 32 .. 63 are turned by 32 columns: then the lanes of a wave, 32 columns of both blocks, read 64 banks
 #pragma unroll
@@ -334,10 +344,15 @@ extern "C" int adaqp_mx4_quantize(const void *x_dev, int64_t ld, int64_t n_rows,
     const int64_t tiles_r = mx_chunks(n_rows) * 2, tiles_c = mx_chunks(n_cols), row_blocks = (n_cols + kMxBlock - 1) / kMxBlock;
     const int64_t blocks = ((codes_t_dev ? tiles_r * tiles_c : (n_rows * row_blocks + kBlock / 2 - 1) / (kBlock / 2)) + 7) / 8 * 8;
     if (blocks > 0x7FFFFFFF) return ADAQP_ESIZE;
-    MxArgs a{x_dev, ld, n_rows, n_cols, (uint32_t)tiles_r, (uint32_t)tiles_c, (uint32_t)row_blocks, seed, codes_dev, scales_dev, codes_t_dev, scales_t_dev, mx_pitch(n_cols),
-             mx_pitch(n_rows)};
     const int64_t bytes = element_bytes(type);
     const int vw = whole_lines(x_dev, ld, bytes) ? (int)(16 / bytes) : vector_elements(x_dev, ld, n_cols, bytes);       // in its own lines a vector may pass the last column
+    int bits = 0;
+    while (((int64_t)1 << bits) < row_blocks) ++bits;
+    const bool below = n_rows * row_blocks + kBlock < ((int64_t)1 << 31);
+    const uint64_t factor = (((uint64_t)1 << (31 + bits)) + row_blocks - 1) / row_blocks;      // at most 2^31 + 1
+    MxArgs a{x_dev, ld, n_rows, n_cols, (uint32_t)tiles_r, (uint32_t)tiles_c, (uint32_t)row_blocks, below ? (uint32_t)factor : 0, (uint32_t)(31 + bits),
+             n_cols % kMxBlock == 0 ? 0 : n_cols % vw ? 1 : 2, seed, codes_dev, scales_dev, codes_t_dev, scales_t_dev, mx_pitch(n_cols),
+             mx_pitch(n_rows)};
     if (type == ADAQP_F32) ADAQP_HIP_TRY((launch_quantize<float>(a, vw, rounding, blocks, (hipStream_t)stream)));
     else                   ADAQP_HIP_TRY((launch_quantize<__bf16>(a, vw, rounding, blocks, (hipStream_t)stream)));
     return ADAQP_OK;
