@@ -38,12 +38,12 @@ typedef enum adaqp_type {
  *   gamma_dev, beta_dev   [dim] fp32; NULL: ones, zeros
  *   stats_dev      [n_rows][2] fp32, written; NULL: not wanted
  * Infinities and NaN give NaN in their own row only.
- * Errors: EINVAL (also: eps negative or not finite, an unknown type, a pointer that is not aligned to its element), EHIP. */
+ * Errors: EINVAL (also: eps negative or not finite, an unknown type, a pointer that is not aligned to its element), ESIZE (more than 2^30 columns), EHIP. */
 int adaqp_layernorm_forward(const void *x_dev, int64_t ldx, int64_t n_rows, int32_t dim, int32_t type,
                             const float *gamma_dev, const float *beta_dev, float eps,
                             void *y_dev, int64_t ldy, float *stats_dev, void *stream);
 
-/* Bytes of workspace adaqp_layernorm_backward needs (a multiple of 256).  Errors: EINVAL. */
+/* Bytes of workspace adaqp_layernorm_backward needs (a multiple of 256).  Errors: EINVAL, ESIZE. */
 int adaqp_layernorm_workspace_bytes(int64_t n_rows, int32_t dim, int64_t *bytes_out);
 
 /* With h_j = (x_j - mean) * rstd and g_j = dy_j * gamma_j, for each row
@@ -53,7 +53,7 @@ int adaqp_layernorm_workspace_bytes(int64_t n_rows, int32_t dim, int64_t *bytes_
  *   dx_dev         NULL: not wanted; may be x or dy (same pitch)
  *   dgamma_dev, dbeta_dev   [dim] fp32, written; both NULL: not wanted (no workspace then); exactly one NULL: EINVAL
  *   workspace_dev  256-byte aligned scratch of at least adaqp_layernorm_workspace_bytes(n_rows, dim)
- * Errors: EINVAL, ESIZE (workspace too small), EHIP. */
+ * Errors: EINVAL, ESIZE (workspace too small, more than 2^30 columns), EHIP. */
 int adaqp_layernorm_backward(const void *x_dev, int64_t ldx, const void *dy_dev, int64_t lddy, int64_t n_rows, int32_t dim, int32_t type,
                              const float *stats_dev, const float *gamma_dev, void *dx_dev, int64_t lddx,
                              float *dgamma_dev, float *dbeta_dev, void *workspace_dev, int64_t workspace_bytes, void *stream);

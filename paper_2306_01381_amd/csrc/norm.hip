@@ -367,6 +367,7 @@ struct NormShape {
 };
 
 constexpr int kLongLanes = 0;
+constexpr int32_t kMostColumns = 1 << 30;       // so that counting them in steps stays within 32 bits
 
 // Lanes per row: the fewest of 8, 16, 32, 64 that have at most four vectors each, then 64 with up to eight, then a workgroup.
 // `cols`: that are read or written.
@@ -500,6 +501,7 @@ extern "C" int adaqp_layernorm_forward(const void *x_dev, int64_t ldx, int64_t n
 {
     if (n_rows < 0 || dim <= 0 || !valid_type(type) || !(eps >= 0.0f && eps <= 3.402823466e+38f)) return ADAQP_EINVAL;
     if (!aligned_to(gamma_dev, 4) || !aligned_to(beta_dev, 4) || !aligned_to(stats_dev, 4)) return ADAQP_EINVAL;
+    if (dim > kMostColumns) return ADAQP_ESIZE;
     if (n_rows == 0) return ADAQP_OK;
     ADAQP_TRY(check_matrix(x_dev, ldx, dim, type));
     ADAQP_TRY(check_matrix(y_dev, ldy, dim, type));
@@ -517,6 +519,7 @@ extern "C" int adaqp_layernorm_forward(const void *x_dev, int64_t ldx, int64_t n
 extern "C" int adaqp_layernorm_workspace_bytes(int64_t n_rows, int32_t dim, int64_t *bytes_out)
 {
     if (!bytes_out || n_rows < 0 || dim <= 0) return ADAQP_EINVAL;
+    if (dim > kMostColumns) return ADAQP_ESIZE;
     const int64_t blocks = n_rows < kMostBlocks ? n_rows : kMostBlocks;
     *bytes_out = (blocks * 2 * dim * 4 + 255) / 256 * 256;
     return ADAQP_OK;
@@ -528,6 +531,7 @@ extern "C" int adaqp_layernorm_backward(const void *x_dev, int64_t ldx, const vo
 {
     if (n_rows < 0 || dim <= 0 || !valid_type(type) || !dgamma_dev != !dbeta_dev) return ADAQP_EINVAL;
     if (!aligned_to(gamma_dev, 4) || !aligned_to(stats_dev, 4) || !aligned_to(dgamma_dev, 4) || !aligned_to(dbeta_dev, 4)) return ADAQP_EINVAL;
+    if (dim > kMostColumns) return ADAQP_ESIZE;
     if (n_rows > 0) {
         if (!stats_dev) return ADAQP_EINVAL;
         ADAQP_TRY(check_matrix(x_dev, ldx, dim, type));

@@ -141,3 +141,25 @@ def test_orthogonalize_definition_is_the_polynomial_of_the_singular_values():
         for a, b, c in STEPS:
             s = a * s + b * s ** 3 + c * s ** 5
         assert np.allclose(D.orthogonalize(g, STEPS, 0.0), u * s @ vt, atol=1e-12)
+
+
+def test_layernorm_refuses_more_columns_than_it_counts():
+    L, n = B.lib(), ctypes.c_int64()
+    many = (1 << 30) + 1
+    assert L.adaqp_layernorm_workspace_bytes(1, many, ctypes.byref(n)) == B.ESIZE
+    assert L.adaqp_layernorm_forward(P, many, 1, many, 0, None, None, 1e-5, P, many, None, None) == B.ESIZE
+    assert L.adaqp_layernorm_backward(P, many, 2 * P, many, 1, many, 0, P, None, 3 * P, many, None, None, None, 0, None) == B.ESIZE
+
+
+def test_wrappers_refuse_tensors_that_are_not_what_they_name():
+    """Found by the binding, before the library is asked."""
+    import torch
+    x = torch.zeros(4, 8)
+    with pytest.raises(TypeError):
+        B.adaqp_layernorm_forward(x, 8, None, None, 1e-5, x)         # not on a device
+    with pytest.raises(TypeError):
+        B.adaqp_mx4_quantize(x, 8, B.MX4_NEAREST, 0, None, None)
+    with pytest.raises(TypeError):
+        B.adaqp_orthogonalize(x, x, STEPS, 1e-7, None)
+    with pytest.raises(ValueError):
+        B._same("call", (3, 0), (4, 0))

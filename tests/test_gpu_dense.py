@@ -513,3 +513,44 @@ def test_calls_follow_their_stream():
         ok = torch.stack([(y == want).all(), (o == turned).all(), (v == values).all(), (q == product).all()])
     stream.synchronize()
     assert ok.cpu().tolist() == [True] * 4 and busy is not None
+
+
+def test_calls_can_be_captured():
+    """One graph of all calls, replayed on inputs that change, between the program's own work: every replay as the calls themselves."""
+    rows, n_in, n_out = 700, 300, 64
+    x, dy = torch.zeros(rows, n_in, device=DEV), torch.zeros(rows, n_out, device=DEV)
+    w4, w4t = B.mx4_empty(n_out, n_in, DEV), B.mx4_empty(n_in, n_out, DEV)
+    B.adaqp_mx4_quantize(torch.randn(n_out, n_in, device=DEV), n_in, B.MX4_NEAREST, 0, w4, w4t)
+    x4, xt4, dz4, dzt4 = (B.mx4_empty(*s, DEV) for s in ((rows, n_in), (n_in, rows), (rows, n_out), (n_out, rows)))
+    z, y, dz, dx = (torch.zeros(rows, c, device=DEV) for c in (n_out, n_out, n_out, n_in))
+    stats, dgamma, dbeta, dw, turned = (torch.zeros(*s, device=DEV) for s in ((rows, 2), (n_out,), (n_out,), (n_out, n_in), (n_out, n_in)))
+    work = _bytes(max(B.adaqp_mx4_matmul_workspace_bytes(rows, n_out, n_in), B.adaqp_mx4_matmul_workspace_bytes(n_out, n_in, rows),
+                      B.adaqp_mx4_matmul_workspace_bytes(rows, n_in, n_out), B.adaqp_layernorm_workspace_bytes(rows, n_out),
+                      B.adaqp_orthogonalize_workspace_bytes(1, n_out, n_in)))
+
+    def calls():
+        B.adaqp_mx4_quantize(x, n_in, B.MX4_NEAREST, 0, x4, xt4)
+        B.adaqp_mx4_matmul(x4, w4, n_in, z, work)
+        B.adaqp_layernorm_forward(z, n_out, None, None, 1e-5, y, stats)
+        B.adaqp_layernorm_backward(z, dy, n_out, stats, None, dz, dgamma, dbeta, work)
+        B.adaqp_mx4_quantize(dz, n_out, B.MX4_STOCHASTIC, 7, dz4, dzt4)
+        B.adaqp_mx4_matmul(dz4, w4t, n_out, dx, work)
+        B.adaqp_mx4_matmul(dzt4, xt4, rows, dw, work)
+        B.adaqp_orthogonalize(dw, turned, STEPS, 1e-7, work)
+
+    x.normal_()
+    dy.normal_()
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for replay in range(4):
+        x.normal_()
+        dy.normal_()
+        graph.replay()
+        got = [t.clone() for t in (y, dgamma, dbeta, dx, dw, turned)]
+        torch.cuda.synchronize()
+        calls()
+        assert all(torch.equal(a, b) for a, b in zip(got, (y, dgamma, dbeta, dx, dw, turned))), replay
+        assert float(turned.abs().sum()) > 0
