@@ -32,6 +32,14 @@ __device__ __forceinline__ void arrived()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(OUTSTANDING) : "memory");
 }
 
+// The same for a wave with a part of the LDS of its own: its loads are there; what it read there is in registers.
+template <int OUTSTANDING>
+__device__ __forceinline__ void own_arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0)" :: "n"(OUTSTANDING) : "memory");
+}
+__device__ __forceinline__ void own_read() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // Which 16 bytes of a line this lane loads with the i-th load of a wave: 8 rows each, the first a multiple of 16.
 __device__ __forceinline__ uint32_t part_of_lane(int i) { return threadIdx.x % 8 ^ (i % 2 * 4 + threadIdx.x % kWave / 16); }
 

@@ -147,14 +147,14 @@ __device__ __forceinline__ float polynomial(const ProductArgs &g, const uint8_t 
 
 constexpr int kSmallTile = 32, kSmallWaves = 8;
 
-// Few tiles: 32 x 32 each, whose eight waves share the lines (w, w + 8, ...) and read them into registers, all at once where there are no more than 16.
-// A product of 256 x 256 x 256 then waits for memory once.
+// Few tiles: 32 x 32 each, whose eight waves share the lines (w, w + 8, ...), each with a part of the LDS of its own and two lines under way: no wave waits for
+// another before the sums are added, and a product of 256 x 256 x 256 waits for memory once.
 template <Product KIND, typename T>
 __global__ __launch_bounds__(kSmallWaves * kWave) void update_small_product_kernel(ProductArgs g)
 {
     constexpr bool kSymmetric = KIND == GRAM || KIND == POLY;
-    constexpr int kLines = 2;                       // under way
-    __shared__ float parts[kSmallWaves][kSmallTile * kSmallTile];
+    constexpr int kStages = 2, kOperand = kSmallTile * kLine, kLoads = 2 * kOperand / (kWave * 16);
+    __shared__ __align__(16) uint8_t lds[kSmallWaves][kStages][2][kOperand];
     __shared__ float tile[kSmallTile][kSmallTile + 1];
     int64_t tr, tc;
     if (kSymmetric) triangle_tile(blockIdx.x, tr, tc);
@@ -164,33 +164,52 @@ __global__ __launch_bounds__(kSmallWaves * kWave) void update_small_product_kern
     }
     const uint8_t *p = g.p + blockIdx.y * g.bytes_p, *q = g.q + blockIdx.y * g.bytes_q;
     const int64_t row0 = tr * kSmallTile, col0 = tc * kSmallTile;
-    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
-    const uint8_t *from_p = p + (row0 + r) * g.pitch + h * 16, *from_q = q + (col0 + r) * g.pitch + h * 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
     sums16 sums;
 #pragma unroll
     for (int e = 0; e < 16; ++e) sums[e] = 0.0f;
-    for (int line = wave; line < (int)g.lines; line += kSmallWaves * kLines) {
-        half8 x[kLines][4], y[kLines][4];           // hi of the two halves of a line, lo of them
+    const uint8_t *from[2] = {p + row0 * g.pitch, q + col0 * g.pitch};
+    uint32_t offset[kLoads / 2];
 #pragma unroll
-        for (int i = 0; i < kLines; ++i) {
-            const int64_t at = (int64_t)min(line + i * kSmallWaves, (int)g.lines - 1) * kLine;
+    for (int i = 0; i < kLoads / 2; ++i) offset[i] = (uint32_t)(i * 8 + lane / 8) * (uint32_t)g.pitch + part_of_lane(i) * 16;
+    auto load = [&](int line, int stage) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                x[i][k] = *reinterpret_cast<const half8 *>(from_p + at + k * 32);
-                y[i][k] = *reinterpret_cast<const half8 *>(from_q + at + k * 32);
-            }
+        for (int o = 0; o < 2; ++o) {
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds_offset(lds[wave][stage][o]));
+#pragma unroll
+            for (int i = 0; i < kLoads / 2; ++i) load_to_lds_16(from[o] + (int64_t)line * kLine, offset[i], to + i * 8 * kLine);
+        }
+    };
+    const int lines = (int)g.lines;
+    auto one = [&](int stage) {
+        const uint8_t *left = lds[wave][stage][0], *right = lds[wave][stage][1];
+        half8 x[4], y[4];                           // hi of the two halves of a line, lo of them
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            x[k] = *reinterpret_cast<const half8 *>(line_part(left, r, k * 2 + h));
+            y[k] = *reinterpret_cast<const half8 *>(line_part(right, r, k * 2 + h));
         }
 #pragma unroll
-        for (int i = 0; i < kLines; ++i) {
-            if (line + i * kSmallWaves >= (int)g.lines) break;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][2 + k], y[i][k], sums, 0, 0, 0);
-                sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][k], y[i][2 + k], sums, 0, 0, 0);
-                sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[i][k], y[i][k], sums, 0, 0, 0);
-            }
+        for (int k = 0; k < 2; ++k) {
+            sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[2 + k], y[k], sums, 0, 0, 0);
+            sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[k], y[2 + k], sums, 0, 0, 0);
+            sums = __builtin_amdgcn_mfma_f32_32x32x16_f16(x[k], y[k], sums, 0, 0, 0);
+        }
+    };
+    if (wave < lines) load(wave, 0);
+    if (wave + kSmallWaves < lines) load(wave + kSmallWaves, 1);
+    int stage = 0;
+    for (int line = wave; line < lines; line += kSmallWaves, stage ^= 1) {
+        if (line + kSmallWaves < lines) own_arrived<kLoads>();
+        else                            own_arrived<0>();
+        one(stage);
+        if (line + 2 * kSmallWaves < lines) {
+            own_read();
+            load(line + 2 * kSmallWaves, stage);
         }
     }
+    own_read();
+    float (*parts)[sizeof(lds[0]) / 4] = reinterpret_cast<float (*)[sizeof(lds[0]) / 4]>(lds);  // a wave's sums lie where its lines were
 #pragma unroll
     for (int e = 0; e < 16; ++e) parts[wave][(e / 4 * 8 + h * 4 + e % 4) * kSmallTile + r] = sums[e];
     __syncthreads();
