@@ -55,47 +55,51 @@ __device__ __forceinline__ double norm_square(const double *partial, int n_parti
     return block_sum((t < n_partial ? partial[t] : 0.0) + (t + kBlock < n_partial ? partial[t + kBlock] : 0.0), lds);
 }
 
-// G / (norm + eps) in units of 2^-power as held matrices: as it lies (`same`) and transposed (`other`), zeros up to the padded sizes.  A workgroup takes 64 x 64.
+// G / (norm + eps) in units of 2^-power as held matrices: as it lies (`same`) and transposed (`other`), zeros up to the padded sizes.  Tiles of 32 x 32, a line of each row
+// of either form: blocks [x] of matrix [y] take turns, a thread four neighbours of a row, then of a column.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void update_split_kernel(const T *g, int64_t ldg, int64_t stride, int64_t n_rows, int64_t n_cols, const double *partial,
                                                               int n_partial, double eps, int power, uint8_t *same, uint8_t *other, int64_t pitch_same,
-                                                              int64_t pitch_other, int64_t held_bytes)
+                                                              int64_t pitch_other, int64_t held_bytes, uint32_t tiles_r, uint32_t tiles_c)
 {
+    constexpr int kTile = 32, kEach = kTile * kTile / kBlock;
     __shared__ double lds[kWavesPerBlock];
-    __shared__ float tile[kPad][kPad + 1];
-    g += blockIdx.z * stride;
-    same += blockIdx.z * held_bytes;
-    other += blockIdx.z * held_bytes;
-    constexpr int kEach = kPad * kPad / kBlock;
-    const int64_t row0 = (int64_t)blockIdx.y * kPad, col0 = (int64_t)blockIdx.x * kPad;
-    const int c = threadIdx.x % kPad, r0 = threadIdx.x / kPad;
-    float v[kEach];
+    __shared__ float tile[2][kTile][kTile + 1];
+    g += blockIdx.y * stride;
+    same += blockIdx.y * held_bytes;
+    other += blockIdx.y * held_bytes;
+    const int major = threadIdx.x / (kTile / kEach), minor = threadIdx.x % (kTile / kEach) * kEach;
+    auto store = [](uint8_t *to, const float (&v)[kEach]) {
+        half4 hi, lo;
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int64_t row = row0 + r0 + i * (kBlock / kPad), col = col0 + c;
-        v[i] = row < n_rows && col < n_cols ? (float)g[row * ldg + col] : 0.0f;
-    }
-    const double total = norm_square(partial + blockIdx.z * n_partial, n_partial, lds);
-    const double scale = ldexp(1.0 / (sqrt(total) + eps), power);
+        for (int k = 0; k < kEach; ++k) {
+            _Float16 a, b;
+            split(v[k], a, b);
+            hi[k] = a;
+            lo[k] = b;
+        }
+        *reinterpret_cast<half4 *>(to) = hi;
+        *reinterpret_cast<half4 *>(to + 64) = lo;
+    };
+    double scale = 0.0;
+    int turn = 0;
+    for (uint32_t at = blockIdx.x; at < tiles_r * tiles_c; at += gridDim.x, turn ^= 1) {
+        const int64_t row0 = (int64_t)(at / tiles_c) * kTile, col0 = (int64_t)(at % tiles_c) * kTile;
+        const int64_t row = row0 + major, col = col0 + minor;
+        float v[kEach];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int r = r0 + i * (kBlock / kPad);
-        const int64_t row = row0 + r, col = col0 + c;
-        v[i] = row < n_rows && col < n_cols ? (float)((double)v[i] * scale) : 0.0f;       // behind the edge also where the scale is not finite
-        tile[r][c] = v[i];
-        _Float16 hi, lo;
-        split(v[i], hi, lo);
-        uint8_t *to = same + held_at(row, col, pitch_same);
-        *reinterpret_cast<_Float16 *>(to) = hi;
-        *reinterpret_cast<_Float16 *>(to + 64) = lo;
-    }
-    __syncthreads();
-    for (int r = threadIdx.x / kPad; r < kPad; r += kBlock / kPad) {
-        _Float16 hi, lo;
-        split(tile[c][r], hi, lo);
-        uint8_t *to = other + held_at(col0 + r, row0 + c, pitch_other);
-        *reinterpret_cast<_Float16 *>(to) = hi;
-        *reinterpret_cast<_Float16 *>(to + 64) = lo;
+        for (int k = 0; k < kEach; ++k) v[k] = (float)g[min(row, n_rows - 1) * ldg + min(col + k, n_cols - 1)];
+        if (at == blockIdx.x) scale = ldexp(1.0 / (sqrt(norm_square(partial + blockIdx.y * n_partial, n_partial, lds)) + eps), power);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            v[k] = row < n_rows && col + k < n_cols ? (float)((double)v[k] * scale) : 0.0f;      // behind the edge also where the scale is not finite
+            tile[turn][major][minor + k] = v[k];
+        }
+        store(same + held_at(row, col, pitch_same), v);
+        __syncthreads();                            // the other tile of the LDS is written next
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) v[k] = tile[turn][minor + k][major];
+        store(other + held_at(col0 + major, row0 + minor, pitch_other), v);
     }
 }
 
@@ -619,7 +623,7 @@ int power_for(double most)
     return kMostPower - e;
 }
 
-constexpr int64_t kFewTiles = 64;                  // of 64 x 64: up to there tiles of 32 x 32 wait less than they read more
+constexpr int64_t kFewTiles = 256;                  // of 32 x 32, one for each CU: up to there they wait less than they read more
 
 template <Product KIND, typename T>
 hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
@@ -634,8 +638,7 @@ hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
         return dim3((uint32_t)(kSymmetric ? (squares_of(g.tiles_r) * kSquare * kSquare * g.parts + 7) / 8 * 8 : tile_blocks(g.tiles_r * g.tiles_c, 1)),
                     (uint32_t)n_matrices);
     };
-    if (tiles(64, 64) <= kFewTiles) {
-        tiles(kSmallTile, kSmallTile);
+    if (tiles(kSmallTile, kSmallTile) <= kFewTiles) {
         const int64_t blocks = kSymmetric ? g.tiles_r * (g.tiles_r + 1) / 2 : g.tiles_r * g.tiles_c;
         update_small_product_kernel<KIND, T><<<dim3((uint32_t)blocks, (uint32_t)n_matrices), kSmallWaves * kWave, 0, st>>>(g);
         return hipGetLastError();
@@ -698,9 +701,10 @@ hipError_t orthogonalize(const T *g, int64_t ldg, int64_t stride_g, T *out, int6
         x[i] = work + u.x_at + 2 * i * n_matrices * u.big;
         xt[i] = x[i] + n_matrices * u.big;
     }
-    update_split_kernel<T><<<dim3((uint32_t)(padded(n_cols) / kPad), (uint32_t)(padded(n_rows) / kPad), (uint32_t)n_matrices), kBlock, 0, st>>>(
+    const int64_t tiles_r = padded(n_rows) / 32, tiles_c = padded(n_cols) / 32, tiles = tiles_r * tiles_c;
+    update_split_kernel<T><<<dim3((uint32_t)(tiles < 2048 ? tiles : 2048), (uint32_t)n_matrices), kBlock, 0, st>>>(
         g, ldg, stride_g, n_rows, n_cols, partial, (int)u.norm_blocks, eps, x_power[0], u.flip ? xt[0] : x[0], u.flip ? x[0] : xt[0],
-        u.flip ? pitch_n : pitch_m, u.flip ? pitch_m : pitch_n, u.big);
+        u.flip ? pitch_n : pitch_m, u.flip ? pitch_m : pitch_n, u.big, (uint32_t)tiles_r, (uint32_t)tiles_c);
     if (hipError_t e = hipGetLastError()) return e;
     for (int32_t s = 0; s < n_steps; ++s) {
         const int now = s % 2;
