@@ -27,6 +27,7 @@ struct MulArgs {
     int64_t chunks;                                 // scale words of a row
     int64_t steps, steps_per_split, splits;
     int64_t tiles_m, tiles_n;
+    bool whole_vectors;                             // rows of out begin and end on 16 bytes
 };
 
 template <int BM, int BN>
@@ -186,10 +187,36 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
     for (; i + STAGES < steps; ++i) one(begin + i, std::true_type());
     for (; i < steps; ++i) one(begin + i, std::false_type());
 
-    // lane's part of a place, and the wave's
-    T *out = (T *)g.out + (split * g.m + row0 + wm) * g.ldo + col0 + wn;
-    const int64_t mine = (int64_t)(h * 4) * g.ldo + r;
+    __builtin_amdgcn_sched_barrier(0);
     const int rows = (int)min(g.m - row0 - wm, (int64_t)BM), cols = (int)min(g.n - col0 - wn, (int64_t)BN), written = (int)min(g.written - col0 - wn, (int64_t)BN);
+    T *out = (T *)g.out + (split * g.m + row0 + wm) * g.ldo + col0 + wn;
+    constexpr int VW = 16 / sizeof(T);
+    if (g.whole_vectors) {
+        // Through the LDS, where the operands were, so that a lane has 16 bytes of a row.
+        constexpr int kSheet = FN * 32, kPitch = kSheet + 8, kLanes = kSheet / VW, kAtOnce = kWave / kLanes;
+        static_assert(sizeof(stage) >= kWavesPerBlock * 32 * kPitch * 4, "the sheets lie where the operands were");
+        float *sheet = reinterpret_cast<float *>(stage) + wave * (32 * kPitch);
+        const int col = lane % kLanes * VW, line = lane / kLanes;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) sheet[(q / 4 * 8 + h * 4 + q % 4) * kPitch + j * 32 + r] = sums[i][j][q];
+#pragma unroll
+            for (int at = 0; at < 32; at += kAtOnce) {
+                float v[VW];
+                load_elements<float, VW>(sheet + (at + line) * kPitch + col, v);
+#pragma unroll
+                for (int k = 0; k < VW; ++k) v[k] = col + k < cols ? v[k] : 0.0f;
+                const int row = i * 32 + at + line;
+                if (row < rows && col < written) store_elements<T, VW, false>(out + row * g.ldo + col, v);
+            }
+        }
+        return;
+    }
+    // lane's part of a place, and the wave's
+    const int64_t mine = (int64_t)(h * 4) * g.ldo + r;
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
@@ -292,9 +319,11 @@ struct MulShape {
     int64_t tiles_m, tiles_n, steps, splits, steps_per_split, bytes;
 };
 
-// Large tiles read less and small ones overlap more: a workgroup of 256 x 256 fills a CU's LDS by itself, so that nothing runs while it begins and ends, and two of
-// 128 x 128 or four of 128 x 64 share one.  us for 8192 x 8192 outputs, k = 1024, 2048, 4096, 8192: 256 x 256 91, 121, 184, 306; 128 x 128 75, 115, 189, 329;
-// 128 x 64 70, 122, 203, 376.  2048 x 2048, k = 2048, 256 tiles of 128 x 128: 14.7 against 13.0 with 128 x 64.
+// Large tiles read less and small ones overlap more: a workgroup of 256 x 256 fills a CU's LDS by itself, so that nothing runs while it begins and ends; two of
+// 128 x 128 or three of 128 x 64 share one.  us for 8192 x 8192 fp32 outputs, k = 256, 1024, 2048, 3200, 4096, 8192: 256 x 256 67, 85, 118, 168, 180, 308;
+// 128 x 128 55, 70, 110, 165, 193, 346; 128 x 64 62, 88, 127, 199, 217, 400.  Where the outputs' edges leave more of a larger tile empty than it gains, the smaller:
+// 196 000 x 300, k = 256, 128 x 128 48 and 128 x 64 44.  A tile's time must not come in two rounds for a bit more than one: 58 000 x 256, k = 602, 908 tiles of
+// 128 x 128, 21.3, with 128 x 64 20.8; 2048 x 2048, k = 2048, 256 tiles of 128 x 128, 14.7 against 13.0.
 // k is split where tiles of 64 x 64 leave half of the CUs idle, in parts of at least eight steps, to about 480 workgroups (256 x 300 outputs, k = 196 000: 12, 24,
 // 50 parts 29, 26, 34 us); from 25 such tiles on, tiles of 128 x 64 with one more step under way (256 x 602, k = 306 000: 70 us, 64 x 64 more than 78).
 MulShape mul_shape(int64_t m, int64_t n, int64_t k)
@@ -321,8 +350,9 @@ MulShape mul_shape(int64_t m, int64_t n, int64_t k)
         split(256 / blocks < most ? 256 / blocks : most);
         return s;
     }
-    if (s.steps >= 12 && tiles(TILE_256_256, 256, 256) >= 512) return s;
-    if (s.steps >= 6 && tiles(TILE_128_128, 128, 128) >= 512) return s;
+    auto padded = [&](int64_t rows, int64_t cols) { return (double)((m + rows - 1) / rows * rows) * (double)((n + cols - 1) / cols * cols); };
+    if (s.steps >= 12 && padded(256, 256) < 1.1 * padded(128, 128) && tiles(TILE_256_256, 256, 256) >= 512) return s;
+    if (padded(128, 128) < 1.1 * padded(128, 64) && tiles(TILE_128_128, 128, 128) >= (s.steps >= 6 ? 512 : 1024)) return s;
     if (tiles(TILE_128_64, 128, 64) >= 256) return s;
     const int64_t small = tiles(TILE_64_64, 64, 64);
     if (small >= 128 || s.steps < 16) return s;
@@ -379,14 +409,17 @@ extern "C" int adaqp_mx4_matmul(const uint8_t *a_codes_dev, const uint8_t *a_sca
         if (workspace_bytes < s.bytes) return ADAQP_ESIZE;
     }
     MulArgs g{a_codes_dev, a_scales_dev, b_codes_dev, b_scales_dev, out_dev, m, n, ldo, 0, mx_pitch(k), mx_chunks(k), s.steps, s.steps_per_split,
-              s.splits, s.tiles_m, s.tiles_n};
+              s.splits, s.tiles_m, s.tiles_n, false};
     const hipStream_t st = (hipStream_t)stream;
     const int64_t line = 128 / element_bytes(type);
     const int64_t written = whole_lines(out_dev, ldo, element_bytes(type)) ? (n + line - 1) / line * line : n;
+    const int64_t vector = 16 / element_bytes(type);
     g.written = s.splits > 1 ? n : written;
+    g.whole_vectors = aligned_to(out_dev, 16) && ldo % vector == 0 && written % vector == 0;
     if (s.splits > 1) {
         g.out = workspace_dev;
         g.ldo = n;
+        g.whole_vectors = n % 4 == 0;
         launch_tiles<float>(g, s, st);
         ADAQP_HIP_TRY(hipGetLastError());
         const int64_t rows = (m + kWavesPerBlock - 1) / kWavesPerBlock;
