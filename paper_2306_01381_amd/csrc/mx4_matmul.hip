@@ -6,6 +6,11 @@
 //
 // Where the tiles are few, k is split over workgroups; the parts' sums, fp32, are added in order by a second kernel.  With at most 32 rows nothing is used
 // twice but those: a workgroup takes 32 columns of out, its eight waves share the lines of k and read them into registers, as many at a time as they can.
+//
+// What bounds it: large products the power that the matrix cores draw.  On random codes they reach 6.1 PFLOP/s from registers alone (9.0 on zeros, at a higher clock);
+// 8192 x 8192 x 4096, fp32 out, 180 us, 3.0 PFLOP/s, of which a tile's loop takes three quarters (35 of 46 us, at 4 PFLOP/s), its first loads 3 and its
+// stores 7.  Shallow products the output: 58 000 x 256, k = 602, 22 us (79 MB, 3.6 TB/s).  Deep ones the operands: 256 x 300, k = 196 000, 30 us and 5 to
+// add up the parts (58 MB).  Few rows their waits: 5 x 8192, k = 4096 and bf16 out, 7 us (17.9 MB, 2.6 TB/s).
 #include "lines.hpp"
 #include "mx4.hpp"
 

@@ -8,6 +8,10 @@
 // every step), and a product is hi hi + hi lo + lo hi, summed in fp32: what is left out is below 2^-22 of a term.  Memory holds lines of 128 bytes: 32 hi,
 // then the 32 lo of the same columns, which is what a step of the products' loop takes of a row.  Both X and its transpose are kept, since the loop
 // runs along rows of both operands.
+//
+// What bounds it: matrices of some hundred rows the chain of launches, each about 4 us from its start over one or two waits for memory to its end (3 of 256 x 256:
+// 17 launches, 70 us; one of 602 x 256 the same); large ones the matrix cores: one of 2048 x 4096 1070 us, 0.84 PFLOP/s counting three fp16 products each (a large
+// fp16 product reaches 1.46).  Its step's products run at 1.0 PFLOP/s (103 GFLOP in 102 us), X X^T in 65 us and 10 to join, A A in 36 and 12.
 #include <math.h>
 
 #include "lines.hpp"
@@ -558,7 +562,7 @@ struct UpdateLayout {
 };
 
 // Cuts of the lines of a symmetric product of n x n: two tiles of 128 x 128 share a CU, and with at least kCutTiles of them there are enough for tiles of that size to
-// pay, but fewer than there is room for.
+// pay, but fewer than there is room for.  us uncut and cut: 2048 x 4096, 136 tiles, X X^T 109 and 75, A A 50 and 47; 1300 x 1300, 66 tiles, 23.5 and 25.5.
 constexpr int kCutTiles = 128, kRoom = 512, kLeastLines = 16;
 
 int update_parts(int64_t n, int64_t lines, int64_t n_matrices)
@@ -623,7 +627,9 @@ int power_for(double most)
     return kMostPower - e;
 }
 
-constexpr int64_t kFewTiles = 256;                  // of 32 x 32, one for each CU: up to there they wait less than they read more
+// Of 32 x 32, one for each CU: up to there they wait less than they read more.  us of 32 x 32 and of 64 x 64: X X^T of 700 x 3000, 253 tiles, 12.9 and 19.2; of
+// 768 x 768, 300 tiles, 9.1 and 8.8; of 1024 x 1024, 528 tiles, 14.9 and 10.4; a step of 640 x 640, 400 tiles, 8.6 and 8.4.
+constexpr int64_t kFewTiles = 256;
 
 template <Product KIND, typename T>
 hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
@@ -643,6 +649,8 @@ hipError_t launch_product(ProductArgs g, int32_t n_matrices, hipStream_t st)
         update_small_product_kernel<KIND, T><<<dim3((uint32_t)blocks, (uint32_t)n_matrices), kSmallWaves * kWave, 0, st>>>(g);
         return hipGetLastError();
     }
+    // The largest tiles that there are enough of for all CUs.  us: a step of 2048 x 4096, 256 x 128 and 128 x 128, 104 and 116; two of 1024 x 2048, 128 x 128 and
+    // 64 x 64, 38.0 and 39.7.  One matrix of 1024 x 1024, 64 x 64 with eight and with four waves, 193 and 206 in all.
     if constexpr (kSymmetric) {
         if (g.parts > 1 || tiles(128, 128) >= 256) {
             tiles(128, 128);

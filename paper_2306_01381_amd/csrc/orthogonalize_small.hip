@@ -1,7 +1,8 @@
 // Orthogonalised updates of matrices that fit a CU's LDS with their products (adaqp_dense.h): one workgroup each does all steps.
 //
 // The same arithmetic as in orthogonalize.hip: operands as two fp16 numbers, three of the four partial products, fp32 sums.  Launched product by product a matrix of
-// 64 x 64 waits 17 times about 4 us for one that takes a tenth of that (66 us); here its five steps need no memory but their input and output.  X is held once, by
+// 64 x 64 waits 17 times about 4 us for products that take a tenth of that (66 us); here its five steps need no memory but their input and output (32 us; 41 x 256 41
+// against 75, 16 x 16 25).  What is left are the waits within a step, for barriers and the LDS.  X is held once, by
 // rows of lines (32 hi, 32 lo); where a product runs along its columns, lanes gather them.  A row's end is 16 bytes apart from the next one's begin modulo 256,
 // so that 16 rows read at one place use all banks.
 #include <math.h>
