@@ -8,8 +8,8 @@
 // twice but those: a workgroup takes 32 columns of out, its eight waves share the lines of k and read them into registers, as many at a time as they can.
 //
 // What bounds it: large products the power that the matrix cores draw.  On random codes they reach 6.1 PFLOP/s from registers alone (9.0 on zeros, at a higher clock);
-// 8192 x 8192 x 4096, fp32 out, 180 us, 3.0 PFLOP/s, of which a tile's loop takes three quarters (35 of 46 us, at 4 PFLOP/s), its first loads 3 and its
-// stores 7.  Shallow products the output: 58 000 x 256, k = 602, 22 us (79 MB, 3.6 TB/s).  Deep ones the operands: 256 x 300, k = 196 000, 30 us and 5 to
+// 8192 x 8192 x 4096, fp32 out, 171 us, 3.2 PFLOP/s, of which a tile's loop takes three quarters (33 of 43 us), its first loads 3 and its
+// stores 7.  Shallow products the output: 58 000 x 256, k = 602, 20 us (79 MB, 3.9 TB/s).  Deep ones the operands: 256 x 300, k = 196 000, 30 us and 5 to
 // add up the parts (58 MB).  Few rows their waits: 5 x 8192, k = 4096 and bf16 out, 7 us (17.9 MB, 2.6 TB/s).
 #include "lines.hpp"
 #include "mx4.hpp"
@@ -99,11 +99,62 @@ struct StepLoads {
     }
 };
 
+// Of a wave's sheet of 32 rows: FN * 32 columns, and the rows 4 apart that a store takes are in different banks.
+constexpr int sheet_pitch(int fn) { return fn * 32 + 8; }
+
+// Stores a wave's sums at (row0, col0); no wave reads operands in `lds` any more.  They go through it, where rows can be stored in vectors, so that a lane has 16 bytes of a
+// row: stored as they are, a tile of 256 x 256 took 10 us for it, fp32 or bf16, and 7 and 5 this way.
+template <typename T, int FM, int FN>
+__device__ __forceinline__ void store_tile(const MulArgs &g, const mx_sums (&sums)[FM][FN], int64_t split, int64_t row0, int64_t col0, float *lds)
+{
+    __builtin_amdgcn_sched_barrier(0);
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+    const int rows = (int)min(g.m - row0, (int64_t)(FM * 32)), cols = (int)min(g.n - col0, (int64_t)(FN * 32)), written = (int)min(g.written - col0, (int64_t)(FN * 32));
+    T *out = (T *)g.out + (split * g.m + row0) * g.ldo + col0;
+    constexpr int VW = 16 / sizeof(T);
+    if (g.whole_vectors) {
+        constexpr int kSheet = FN * 32, kPitch = sheet_pitch(FN), kLanes = kSheet / VW, kAtOnce = kWave / kLanes;
+        float *sheet = lds + wave * (32 * kPitch);
+        const int col = lane % kLanes * VW, line = lane / kLanes;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) sheet[(q / 4 * 8 + h * 4 + q % 4) * kPitch + j * 32 + r] = sums[i][j][q];
+#pragma unroll
+            for (int at = 0; at < 32; at += kAtOnce) {
+                float v[VW];
+                load_elements<float, VW>(sheet + (at + line) * kPitch + col, v);
+#pragma unroll
+                for (int k = 0; k < VW; ++k) v[k] = col + k < cols ? v[k] : 0.0f;
+                const int row = i * 32 + at + line;
+                if (row < rows && col < written) store_elements<T, VW, false>(out + row * g.ldo + col, v);
+            }
+        }
+        return;
+    }
+    // lane's part of a place, and the wave's
+    const int64_t mine = (int64_t)(h * 4) * g.ldo + r;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+            const int row = i * 32 + q / 4 * 8 + q % 4;
+            if (row + h * 4 >= rows) continue;
+            T *to = out + row * g.ldo + mine;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                if (j * 32 + r < written) to[j * 32] = j * 32 + r < cols ? (T)sums[i][j][q] : (T)0.0f;
+        }
+}
+
 template <typename T, int BM, int BN, int STAGES>
 __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
 {
     constexpr int FM = BM / 64, FN = BN / 64;       // 32 x 32 parts of a wave
     __shared__ Stage<BM, BN> stage[STAGES];
+    static_assert(sizeof(stage) >= kWavesPerBlock * 32 * sheet_pitch(FN) * 4, "the sheets lie where the operands were");
     using Loads = StepLoads<BM, BN>;
     const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
     if (place.part < 0) return;
@@ -192,47 +243,170 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
     for (; i + STAGES < steps; ++i) one(begin + i, std::true_type());
     for (; i < steps; ++i) one(begin + i, std::false_type());
 
-    __builtin_amdgcn_sched_barrier(0);
-    const int rows = (int)min(g.m - row0 - wm, (int64_t)BM), cols = (int)min(g.n - col0 - wn, (int64_t)BN), written = (int)min(g.written - col0 - wn, (int64_t)BN);
-    T *out = (T *)g.out + (split * g.m + row0 + wm) * g.ldo + col0 + wn;
-    constexpr int VW = 16 / sizeof(T);
-    if (g.whole_vectors) {
-        // Through the LDS, where the operands were, so that a lane has 16 bytes of a row.
-        constexpr int kSheet = FN * 32, kPitch = kSheet + 8, kLanes = kSheet / VW, kAtOnce = kWave / kLanes;
-        static_assert(sizeof(stage) >= kWavesPerBlock * 32 * kPitch * 4, "the sheets lie where the operands were");
-        float *sheet = reinterpret_cast<float *>(stage) + wave * (32 * kPitch);
-        const int col = lane % kLanes * VW, line = lane / kLanes;
+    store_tile<T, FM, FN>(g, sums, split, row0 + wm, col0 + wn, reinterpret_cast<float *>(stage));
+}
+
+// The same in steps of half a line, 128 columns and one scale word.  Of tiles of 256 x 256 two steps of a line fit the LDS, and the loads of the next would have to follow one another
+// in a quarter of a step if they were to arrive in the rest; of half a line four fit, and loads and reads of the LDS alike lie one by one between the products
+// (8192 x 8192 x 4096 fp32 181 us in lines, 176 with the loads spread, 171 with the reads spread).  Short rows have less of an empty half line.
+template <int BM, int BN>
+struct HalfStage {
+    uint8_t a[BM * kLine / 2], b[BN * kLine / 2];
+    uint32_t scales[BM + BN];
+};
+
+// Of such lines the four 16-byte parts lie at (part ^ row / 4 mod 4): four rows fill the banks.
+__device__ __forceinline__ const uint8_t *half_part(const uint8_t *lds, int row, int part) { return lds + row * (kLine / 2) + (part ^ row / 4 % 4) * 16; }
+
+template <int BM, int BN>
+struct HalfLoads {
+    static constexpr int kA = BM / 64, kB = BN / 64, kScaleLoads = (BM + BN + kBlock - 1) / kBlock, kLoads = kA + kB + kScaleLoads;
+    uint32_t a[kA], b[kB], scale[kScaleLoads];
+    const uint8_t *from_a, *from_b, *from_scale[kScaleLoads];
+    int64_t scale_stride[kScaleLoads];
+    uint32_t to_scale[kScaleLoads];
+    int wave;
+
+    __device__ __forceinline__ HalfLoads(const MulArgs &g, int64_t row0, int64_t col0, int64_t begin)
+    {
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+        const int lane = threadIdx.x % kWave;
+        from_a = g.a_codes + row0 * g.pitch + begin * (kLine / 2);
+        from_b = g.b_codes + col0 * g.pitch + begin * (kLine / 2);
+        auto places = [&](auto &to, int rows, int64_t left) {           // 16 rows of four parts a load
+            const uint32_t last = (uint32_t)min((int64_t)rows, left) - 1;
 #pragma unroll
-        for (int i = 0; i < FM; ++i) {
+            for (int i = 0; i < rows / 64; ++i) to[i] = min((uint32_t)(wave * (rows / 4) + i * 16 + lane / 4), last) * (uint32_t)g.pitch + (lane % 4 ^ lane / 16) * 16;
+        };
+        places(a, BM, g.m - row0);
+        places(b, BN, g.n - col0);
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-#pragma unroll
-                for (int q = 0; q < 16; ++q) sheet[(q / 4 * 8 + h * 4 + q % 4) * kPitch + j * 32 + r] = sums[i][j][q];
-#pragma unroll
-            for (int at = 0; at < 32; at += kAtOnce) {
-                float v[VW];
-                load_elements<float, VW>(sheet + (at + line) * kPitch + col, v);
-#pragma unroll
-                for (int k = 0; k < VW; ++k) v[k] = col + k < cols ? v[k] : 0.0f;
-                const int row = i * 32 + at + line;
-                if (row < rows && col < written) store_elements<T, VW, false>(out + row * g.ldo + col, v);
-            }
+        for (int i = 0; i < kScaleLoads; ++i) {
+            int at = (i * kWavesPerBlock + wave) * kWave % (BM + BN);
+            to_scale[i] = at * 4;
+            const bool of_b = at >= BM;
+            at -= of_b ? BM : 0;
+            const int64_t n = of_b ? g.n : g.m, first = of_b ? col0 : row0;
+            scale_stride[i] = n * 4;
+            from_scale[i] = (of_b ? g.b_scales : g.a_scales) + (begin * n + first) * 4;
+            scale[i] = min((uint32_t)(at + lane), (uint32_t)min((int64_t)(of_b ? BN : BM), n - first) - 1) * 4;
         }
-        return;
     }
-    // lane's part of a place, and the wave's
-    const int64_t mine = (int64_t)(h * 4) * g.ldo + r;
+
+    __device__ __forceinline__ void load(int i, int step, const HalfStage<BM, BN> &s) const
+    {
+        if (i < kA)           load_to_lds_16(from_a + (int64_t)step * (kLine / 2), a[i], __builtin_amdgcn_readfirstlane(lds_offset(s.a) + (wave * (BM / 4) + i * 16) * (kLine / 2)));
+        else if (i < kA + kB) load_to_lds_16(from_b + (int64_t)step * (kLine / 2), b[i - kA], __builtin_amdgcn_readfirstlane(lds_offset(s.b) + (wave * (BN / 4) + (i - kA) * 16) * (kLine / 2)));
+        else                  load_to_lds_4(from_scale[i - kA - kB] + step * scale_stride[i - kA - kB], scale[i - kA - kB], lds_offset(s.scales) + to_scale[i - kA - kB]);
+    }
+};
+
+template <typename T, int BM, int BN, int STAGES>
+__global__ __launch_bounds__(kBlock) void mx4_matmul_halves_kernel(MulArgs g)
+{
+    constexpr int FM = BM / 64, FN = BN / 64;
+    __shared__ HalfStage<BM, BN> stage[STAGES];
+    static_assert(sizeof(stage) >= kWavesPerBlock * 32 * sheet_pitch(FN) * 4, "the sheets lie where the operands were");
+    using Loads = HalfLoads<BM, BN>;
+    const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
+    if (place.part < 0) return;
+    const int64_t row0 = place.row * BM, col0 = place.col * BN;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
+    const int wm = wave / 2 * (BM / 2), wn = wave % 2 * (BN / 2);
+    const int64_t begin = place.part * g.steps_per_split * kStepChunks;
+    const int steps = (int)min(g.steps_per_split * kStepChunks, g.chunks - begin);
+    const Loads loads(g, row0, col0, begin);
+
+    mx_sums sums[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-            const int row = i * 32 + q / 4 * 8 + q % 4;
-            if (row + h * 4 >= rows) continue;
-            T *to = out + row * g.ldo + mine;
+        for (int j = 0; j < FN; ++j)
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-                if (j * 32 + r < written) to[j * 32] = j * 32 + r < cols ? (T)sums[i][j][q] : (T)0.0f;
-        }
+            for (int q = 0; q < 16; ++q) sums[i][j][q] = 0.0f;
+
+    struct Part { int4 a[FM], b[FN]; } part[2];     // of 64 columns
+    uint32_t next_a[FM], next_b[FN], sa[FM], sb[FN];
+    // Read `i` of a part, in the order in which products need them.
+    constexpr int kReads = FM + FN;
+    auto read = [&](const HalfStage<BM, BN> &s, int at, int i, Part &to) {
+        if (i == 0)       to.a[0] = *reinterpret_cast<const int4 *>(half_part(s.a, wm + r, at * 2 + h));
+        else if (i <= FN) to.b[i - 1] = *reinterpret_cast<const int4 *>(half_part(s.b, wn + (i - 1) * 32 + r, at * 2 + h));
+        else              to.a[i - FN] = *reinterpret_cast<const int4 *>(half_part(s.a, wm + (i - FN) * 32 + r, at * 2 + h));
+    };
+    auto read_scales = [&](const HalfStage<BM, BN> &s) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) next_a[i] = s.scales[wm + i * 32 + r];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) next_b[j] = s.scales[BM + wn + j * 32 + r];
+    };
+    auto multiply = [&](const Part &f, int at, auto between) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const mx_codes a{f.a[i].x, f.a[i].y, f.a[i].z, f.a[i].w, 0, 0, 0, 0}, b{f.b[j].x, f.b[j].y, f.b[j].z, f.b[j].w, 0, 0, 0, 0};
+                sums[i][j] = at == 0 ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sums[i][j], 4, 4, 0, (int)sa[i], 0, (int)sb[j])
+                                     : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, sums[i][j], 4, 4, 2, (int)sa[i], 2, (int)sb[j]);
+                between(i * FN + j);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // Up to STAGES steps are under way.  A step's second part is multiplied behind the barrier after which the next step is in the LDS and its own buffer free; the loads into
+    // that buffer are spread over those products and the first of the next step.
+    constexpr int kProducts = FM * FN, kFirst = Loads::kLoads / 2, kReadsAtOnce = (kReads + kProducts - 1) / kProducts;
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s)
+        if (s < steps)
+#pragma unroll
+            for (int l = 0; l < (s < STAGES - 1 ? Loads::kLoads : kFirst); ++l) loads.load(l, s, stage[s]);
+    if (steps >= STAGES) arrived<Loads::kLoads * (STAGES - 2) + kFirst>();
+    else                 arrived<0>();
+    read_scales(stage[0]);
+#pragma unroll
+    for (int i = 0; i < kReads; ++i) read(stage[0], 0, i, part[0]);
+    int now = 0, before = STAGES - 1;
+    auto one = [&](int step, auto pending, auto more) {
+        constexpr bool kPending = decltype(pending)::value, kMore = decltype(more)::value;
+        const HalfStage<BM, BN> &s = stage[now], &last = stage[before];
+        before = now;
+        now = now + 1 == STAGES ? 0 : now + 1;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = next_a[i] >> (8 * h);      // the upper half of a wave has the odd blocks
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sb[j] = next_b[j] >> (8 * h);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(part[0], 0, [&](int p) {
+#pragma unroll
+            for (int i = p * kReadsAtOnce; i < (p + 1) * kReadsAtOnce && i < kReads; ++i) read(s, 1, i, part[1]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kPending) {
+#pragma unroll
+                for (int l = kFirst + p * (Loads::kLoads - kFirst) / kProducts; l < kFirst + (p + 1) * (Loads::kLoads - kFirst) / kProducts; ++l)
+                    loads.load(l, step - 1 + STAGES, last);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+        arrived<kPending ? Loads::kLoads * (STAGES - 2) : 0>();
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(part[1], 1, [&](int p) {
+#pragma unroll
+            for (int i = p * kReadsAtOnce; i < (p + 1) * kReadsAtOnce && i < kReads; ++i) read(stage[now], 0, i, part[0]);
+            if (p == kProducts / 2) read_scales(stage[now]);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kMore) {
+#pragma unroll
+                for (int l = p * kFirst / kProducts; l < (p + 1) * kFirst / kProducts; ++l) loads.load(l, step + STAGES, s);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        });
+    };
+    int step = 0;
+    for (; step + STAGES < steps; ++step) one(step, std::true_type(), std::true_type());
+    if (steps >= STAGES) one(step++, std::true_type(), std::false_type());
+    for (; step < steps; ++step) one(step, std::false_type(), std::false_type());
+    store_tile<T, FM, FN>(g, sums, place.part, row0 + wm, col0 + wn, reinterpret_cast<float *>(stage));
 }
 
 constexpr int kFewRows = 32, kFewWaves = 8;
@@ -317,7 +491,7 @@ __global__ __launch_bounds__(kBlock) void mx4_join_kernel(const float *parts, in
     }
 }
 
-enum MulTile { FEW_ROWS, TILE_64_64, TILE_128_64, TILE_128_64_DEEP, TILE_128_128, TILE_256_256 };
+enum MulTile { FEW_ROWS, TILE_64_64, TILE_128_64, TILE_128_64_HALVES, TILE_128_64_DEEP, TILE_128_128, TILE_256_256 };
 
 struct MulShape {
     MulTile tile;
@@ -325,10 +499,10 @@ struct MulShape {
 };
 
 // Large tiles read less and small ones overlap more: a workgroup of 256 x 256 fills a CU's LDS by itself, so that nothing runs while it begins and ends; two of
-// 128 x 128 or three of 128 x 64 share one.  us for 8192 x 8192 fp32 outputs, k = 256, 1024, 2048, 3200, 4096, 8192: 256 x 256 67, 85, 118, 168, 180, 308;
+// 128 x 128 or three of 128 x 64 share one.  us for 8192 x 8192 fp32 outputs, k = 256, 1024, 2048, 3200, 4096, 8192: 256 x 256 67, 86, 113, 160, 171, 293;
 // 128 x 128 55, 70, 110, 165, 193, 346; 128 x 64 62, 88, 127, 199, 217, 400.  Where the outputs' edges leave more of a larger tile empty than it gains, the smaller:
 // 196 000 x 300, k = 256, 128 x 128 48 and 128 x 64 44.  A tile's time must not come in two rounds for a bit more than one: 58 000 x 256, k = 602, 908 tiles of
-// 128 x 128, 21.3, with 128 x 64 20.8; 2048 x 2048, k = 2048, 256 tiles of 128 x 128, 14.7 against 13.0.
+// 128 x 128, 21.3, with 128 x 64 19.6 (in whole lines 21.0; 8192 x 8192, k = 1024, 107 and 107, k = 2048 in half lines 144, in whole ones 129); 2048 x 2048, k = 2048, 256 tiles of 128 x 128, 14.7 against 13.0.
 // k is split where tiles of 64 x 64 leave half of the CUs idle, in parts of at least eight steps, to about 480 workgroups (256 x 300 outputs, k = 196 000: 12, 24,
 // 50 parts 29, 26, 34 us); from 25 such tiles on, tiles of 128 x 64 with one more step under way (256 x 602, k = 306 000: 70 us, 64 x 64 more than 78).
 MulShape mul_shape(int64_t m, int64_t n, int64_t k)
@@ -358,7 +532,7 @@ MulShape mul_shape(int64_t m, int64_t n, int64_t k)
     auto padded = [&](int64_t rows, int64_t cols) { return (double)((m + rows - 1) / rows * rows) * (double)((n + cols - 1) / cols * cols); };
     if (s.steps >= 12 && padded(256, 256) < 1.1 * padded(128, 128) && tiles(TILE_256_256, 256, 256) >= 512) return s;
     if (padded(128, 128) < 1.1 * padded(128, 64) && tiles(TILE_128_128, 128, 128) >= (s.steps >= 6 ? 512 : 1024)) return s;
-    if (tiles(TILE_128_64, 128, 64) >= 256) return s;
+    if (tiles(s.steps <= 3 ? TILE_128_64_HALVES : TILE_128_64, 128, 64) >= 256) return s;
     const int64_t small = tiles(TILE_64_64, 64, 64);
     if (small >= 128 || s.steps < 16) return s;
     const int64_t blocks = small >= 25 ? tiles(TILE_128_64_DEEP, 128, 64) : small;
@@ -374,9 +548,10 @@ void launch_tiles(const MulArgs &g, const MulShape &s, hipStream_t st)
         case FEW_ROWS:         mx4_few_rows_kernel<T><<<dim3((uint32_t)((g.written + 31) / 32), (uint32_t)s.splits), kFewWaves * kWave, 0, st>>>(g); break;
         case TILE_64_64:       mx4_matmul_kernel<T, 64, 64, 4><<<blocks, kBlock, 0, st>>>(g); break;
         case TILE_128_64:      mx4_matmul_kernel<T, 128, 64, 2><<<blocks, kBlock, 0, st>>>(g); break;
+        case TILE_128_64_HALVES: mx4_matmul_halves_kernel<T, 128, 64, 4><<<blocks, kBlock, 0, st>>>(g); break;
         case TILE_128_64_DEEP: mx4_matmul_kernel<T, 128, 64, 3><<<blocks, kBlock, 0, st>>>(g); break;
         case TILE_128_128:     mx4_matmul_kernel<T, 128, 128, 2><<<blocks, kBlock, 0, st>>>(g); break;
-        case TILE_256_256:     mx4_matmul_kernel<T, 256, 256, 2><<<blocks, kBlock, 0, st>>>(g); break;
+        case TILE_256_256:     mx4_matmul_halves_kernel<T, 256, 256, 4><<<blocks, kBlock, 0, st>>>(g); break;
     }
 }
 
