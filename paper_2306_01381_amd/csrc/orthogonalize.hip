@@ -10,8 +10,9 @@
 // runs along rows of both operands.
 //
 // What bounds it: matrices of some hundred rows the chain of launches, each about 4 us from its start over one or two waits for memory to its end (3 of 256 x 256:
-// 17 launches, 70 us; one of 602 x 256 the same); large ones the matrix cores: one of 2048 x 4096 1070 us, 0.84 PFLOP/s counting three fp16 products each (a large
-// fp16 product reaches 1.46).  Its step's products run at 1.0 PFLOP/s (103 GFLOP in 102 us), X X^T in 65 us and 10 to join, A A in 36 and 12.
+// 17 launches, 70 us; one of 602 x 256 the same); large ones the matrix cores: one of 2048 x 4096 1036 us, 0.87 PFLOP/s counting three fp16 products each (a large
+// fp16 product reaches 1.46).  Its step's products run at 1.1 PFLOP/s (103 GFLOP in 96 us), X X^T in 63 us and 10 to join, A A in 35 and 12; of zeros, which draw less, it
+// takes 850.
 #include <math.h>
 
 #include "lines.hpp"
@@ -397,19 +398,18 @@ __global__ __launch_bounds__(kBlock * GROUPS) void update_product_kernel(Product
         if (i < kLoadsP) of_p.template load<false>(i, from_p + (int64_t)line * (kLine * GROUPS), TileLoads<TR>::place(s.p));
         else             of_q.template load<false>(i - kLoadsP, from_q + (int64_t)line * (kLine * GROUPS), TileLoads<TC>::place(s.q));
     };
-    // The operands of half a line, 16 columns: read from the LDS while the half before is multiplied.
+    // The operands of half a line, 16 columns: read from the LDS while the half before is multiplied, one by one between its products, in the order in which they
+    // are needed (2048 x 4096 1080 us with them in a row before the products).
     struct Half { half8 ph[FR], pl[FR], qh[FC], ql[FC]; } half[2];
-    auto read = [&](const auto &s, int k, Half &to) {
-#pragma unroll
-        for (int i = 0; i < FR; ++i) {
-            to.ph[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, k * 2 + h));
-            to.pl[i] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + i * 32 + r, 4 + k * 2 + h));
-        }
-#pragma unroll
-        for (int j = 0; j < FC; ++j) {
-            to.qh[j] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + j * 32 + r, k * 2 + h));
-            to.ql[j] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + j * 32 + r, 4 + k * 2 + h));
-        }
+    constexpr int kReads = 2 * (FR + FC);
+    auto read = [&](const auto &s, int k, int i, Half &to) {
+        const bool second = i >= FR + FC;           // hi of p and lo of q
+        i -= second ? FR + FC : 0;
+        if (i == 0 || i > FC) {
+            const int row = i == 0 ? 0 : i - FC;
+            (second ? to.ph : to.pl)[row] = *reinterpret_cast<const half8 *>(line_part(s.p, wr + row * 32 + r, (second ? 0 : 4) + k * 2 + h));
+        } else
+            (second ? to.ql : to.qh)[i - 1] = *reinterpret_cast<const half8 *>(line_part(s.q, wc + (i - 1) * 32 + r, (second ? 4 : 0) + k * 2 + h));
     };
     // `between(i)` is done behind product i of the half's 3 FR FC.
     auto multiply = [&](const Half &f, auto between) {
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(kBlock * GROUPS) void update_product_kernel(Product
     // Up to STAGES lines are under way.  A line's second half is multiplied behind the barrier after which the next line is in the LDS and its own buffer
     // free; the loads into that buffer are spread over that half's products and those of the next line's first half.  No branches: across one the compiler
     // would take products to the other side of the barrier.
-    constexpr int kProducts = 3 * FR * FC, kFirst = kLoads / 2;         // loads behind the products of a second half
+    constexpr int kProducts = 3 * FR * FC, kReadsAtOnce = (kReads + kProducts - 1) / kProducts, kFirst = kLoads / 2;   // loads behind the products of a second half
 #pragma unroll
     for (int s = 0; s < STAGES; ++s)
         if (s < lines)
@@ -436,16 +436,19 @@ __global__ __launch_bounds__(kBlock * GROUPS) void update_product_kernel(Product
             for (int l = 0; l < (s < STAGES - 1 ? kLoads : kFirst); ++l) load(l, s, stage[s]);
     if (lines >= STAGES) arrived<kLoads * (STAGES - 2) + kFirst>();
     else                 arrived<0>();
-    read(stage[0], 0, half[0]);
+#pragma unroll
+    for (int i = 0; i < kReads; ++i) read(stage[0], 0, i, half[0]);
     int now = 0, before = STAGES - 1;
     auto one = [&](int line, auto pending, auto more) {
         constexpr bool kPending = decltype(pending)::value, kMore = decltype(more)::value;
         const Stage &s = stage[now], &last = stage[before];
         before = now;
         now = now + 1 == STAGES ? 0 : now + 1;
-        read(s, 1, half[1]);
         __builtin_amdgcn_sched_barrier(0);
         multiply(half[0], [&](int i) {
+#pragma unroll
+            for (int at = i * kReadsAtOnce; at < (i + 1) * kReadsAtOnce && at < kReads; ++at) read(s, 1, at, half[1]);
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (kPending) {
 #pragma unroll
                 for (int l = kFirst + i * (kLoads - kFirst) / kProducts; l < kFirst + (i + 1) * (kLoads - kFirst) / kProducts; ++l) load(l, line - 1 + STAGES, last);
@@ -453,9 +456,11 @@ __global__ __launch_bounds__(kBlock * GROUPS) void update_product_kernel(Product
             }
         });
         arrived<kPending ? kLoads * (STAGES - 2) : 0>();
-        read(stage[now], 0, half[0]);
         __builtin_amdgcn_sched_barrier(0);
         multiply(half[1], [&](int i) {
+#pragma unroll
+            for (int at = i * kReadsAtOnce; at < (i + 1) * kReadsAtOnce && at < kReads; ++at) read(stage[now], 0, at, half[0]);
+            __builtin_amdgcn_sched_barrier(0);
             if constexpr (kMore) {
 #pragma unroll
                 for (int l = i * kFirst / kProducts; l < (i + 1) * kFirst / kProducts; ++l) load(l, line + STAGES, s);
