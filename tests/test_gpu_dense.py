@@ -355,6 +355,34 @@ def test_mx4_matmul_of_every_tile(m, n, k):
     assert bool(((out.double() - want).abs() <= 2 * U * (k / 64 + 16) * size).all())
 
 
+@pytest.mark.parametrize("m,n,k", [(9000, 300, 40), (9001, 301, 500), (8999, 260, 640), (9000, 300, 1000), (8200, 2050, 130), (8190, 2052, 512), (8200, 4090, 2900)])
+@pytest.mark.parametrize("kind", sorted(TYPES))
+@pytest.mark.parametrize("pad", [0, 3, 64])
+def test_mx4_matmul_stores_what_is_there(m, n, k, kind, pad):
+    """Many rows of short and long lines, out with rows that begin anywhere, on vectors and on whole lines: products in float64 of the values, nothing else touched."""
+    _say("mx4 matmul stores", m, n, k, kind, pad)
+    dtype = TYPES[kind]
+    gen = torch.Generator(device=DEV).manual_seed(m + k)
+    packed, values = [], []
+    for rows in (m, n):
+        x = torch.randn(rows, k, generator=gen, device=DEV)
+        packed.append(B.mx4_empty(rows, k, DEV))
+        B.adaqp_mx4_quantize(x, k, B.MX4_NEAREST, 0, packed[-1], None)
+        values.append(torch.from_numpy(D.mx4_values(packed[-1][0].cpu().numpy(), packed[-1][1].cpu().numpy(), k)).to(DEV))
+    ld = n + 3 if pad == 3 else -(-n // pad) * pad if pad else n
+    buf = torch.full((m * ld + 64,), SENTINEL, dtype=dtype, device=DEV)
+    out = buf[:m * ld].view(m, ld)
+    B.adaqp_mx4_matmul(*packed, k, out[:, :n], _bytes(B.adaqp_mx4_matmul_workspace_bytes(m, n, k)).fill_(0xFF))
+    want, size = values[0] @ values[1].t(), values[0].abs() @ values[1].abs().t()
+    tol = 2 * U * (k / 64 + 16) * size
+    if kind == "bf16":
+        tol = tol + 2.0 ** -8 * (want.abs() + tol)
+    assert bool(((out[:, :n].double() - want).abs() <= tol).all())
+    line = 128 // dtype.itemsize
+    written = -(-n // line) * line if ld % line == 0 else n         # whole lines, zeros behind the last column
+    assert not out[:, n:written].any() and bool((out[:, written:] == SENTINEL).all()) and bool((buf[m * ld:] == SENTINEL).all())
+
+
 def test_mx4_matmul_of_extreme_scales_nan_blocks_and_nothing():
     (ac, asc), av = _mx_random(40, 200, 1)
     (bc, bsc), bv = _mx_random(50, 200, 2)
