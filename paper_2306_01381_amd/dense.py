@@ -50,20 +50,25 @@ class DenseLayer:
                    B.adaqp_orthogonalize_workspace_bytes(1, n_out, n_in), 1)
         self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)       # of one call at a time: they follow one another on a stream
         self.steps = 0
+        self.trained_on = False                     # whether xt4 is of the last forward's x
         self._quantize_weight()
 
     def _quantize_weight(self) -> None:
         B.adaqp_mx4_quantize(self.weight, self.n_in, B.MX4_NEAREST, 0, self.w4, self.wt4)
 
     def forward(self, x: torch.Tensor, training: bool = True) -> torch.Tensor:
-        """y of x [n_rows, n_in].  `training`: backward will follow, so that the columns' form of x is made in the same pass."""
+        """y of x [n_rows, n_in].  `training`: backward may follow, so that the columns' form of x is made in the same pass."""
+        self.trained_on = False
         B.adaqp_mx4_quantize(x, self.n_in, B.MX4_NEAREST, 0, self.x4, self.xt4 if training else None)
         B.adaqp_mx4_matmul(self.x4, self.w4, self.n_in, self.z, self.workspace)
         B.adaqp_layernorm_forward(self.z, self.n_out, self.gamma, self.beta, self.eps, self.y, self.stats)
+        self.trained_on = training
         return self.y
 
     def backward(self, dy: torch.Tensor, wants_dx: bool = True) -> Optional[torch.Tensor]:
-        """dx of the last forward(), and the parameters' gradients in dweight, dgamma and dbeta."""
+        """dx of the last forward(), and the parameters' gradients in dweight, dgamma and dbeta.  Raises if that was none for training."""
+        if not self.trained_on:
+            raise RuntimeError("backward() needs a forward(training=True) before it: there is no columns' form of x")
         B.adaqp_layernorm_backward(self.z, dy, self.n_out, self.stats, self.gamma, self.dz, self.dgamma, self.dbeta, self.workspace)
         self.steps += 1
         B.adaqp_mx4_quantize(self.dz, self.n_out, B.MX4_STOCHASTIC, self.seed + 2 * self.steps, self.dz4 if wants_dx else None, self.dzt4)
