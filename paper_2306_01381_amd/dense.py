@@ -7,6 +7,7 @@ Everything computational happens inside libadaqp; this module only owns memory a
 """
 from __future__ import annotations
 
+import itertools
 import math
 from typing import Optional
 
@@ -17,6 +18,9 @@ from . import binding as B
 # (a, b, c) of the update's steps: five times s -> a s + b s^3 + c s^5 takes singular values from a hundredth of the norm on to between 0.7 and 1.2.
 UPDATE_STEPS = ((3.4445, -4.7750, 2.0315),) * 5
 
+_layers = itertools.count()
+_APART = 0x9E3779B97F4A7C15                         # odd, about 2^64 over the golden ratio: multiples of it by near numbers lie far apart
+
 
 def rows_of_lines(n_rows: int, n_cols: int, device, dtype=torch.float32) -> torch.Tensor:
     """An uninitialised [n_rows, n_cols] matrix whose rows cover whole 128-byte lines."""
@@ -25,8 +29,13 @@ def rows_of_lines(n_rows: int, n_cols: int, device, dtype=torch.float32) -> torc
 
 
 class DenseLayer:
-    def __init__(self, n_rows: int, n_in: int, n_out: int, device="cuda:0", seed: int = 0, eps: float = 1e-5, weight: Optional[torch.Tensor] = None):
-        self.n_rows, self.n_in, self.n_out, self.eps, self.seed = n_rows, n_in, n_out, eps, seed
+    def __init__(self, n_rows: int, n_in: int, n_out: int, device="cuda:0", seed: Optional[int] = None, eps: float = 1e-5, weight: Optional[torch.Tensor] = None):
+        """`seed`: of the weights and of the numbers that round gradients; layers that are trained together need different ones.  None: how many
+        layers were made without one before this."""
+        if seed is None:
+            seed = next(_layers)
+        self.n_rows, self.n_in, self.n_out, self.eps = n_rows, n_in, n_out, eps
+        self.seed = seed * _APART % 2 ** 64         # of the rounding numbers; every step takes two more
         self.device = torch.device(device)
         if weight is None:
             gen = torch.Generator().manual_seed(seed)

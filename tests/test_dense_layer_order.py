@@ -43,3 +43,29 @@ def test_backward_wants_the_columns_of_its_own_forward(calls):
     layer.forward(x)
     layer.backward(dy)
     assert layer.steps == 3
+
+
+def test_layers_round_by_numbers_of_their_own(calls):
+    """A gradient that one layer rounded is what the next rounds again: with the same numbers its error would not be independent.  The numbers of a call are those of its
+    seed (rows) and the one behind it (columns)."""
+    def taken(layer, steps=200):
+        layer.forward(torch.zeros(20, 8))
+        calls.clear()
+        for _ in range(steps):
+            layer.backward(torch.zeros(20, 8))
+        seeds = [args[3] % 2 ** 64 for name, args in calls if name == "adaqp_mx4_quantize"]
+        assert len(seeds) == steps
+        return {s for seed in seeds for s in (seed, (seed + 1) % 2 ** 64)}
+
+    sets = [taken(DenseLayer(20, 8, 8, "cpu")) for _ in range(4)] + [taken(DenseLayer(20, 8, 8, "cpu", seed=s)) for s in (1 << 40, (1 << 40) + 1, (1 << 40) + 3, 2 ** 63 - 1)]
+    assert all(len(s) == 400 for s in sets)
+    for i, a in enumerate(sets):
+        for b in sets[:i]:
+            assert not a & b
+    assert taken(DenseLayer(20, 8, 8, "cpu", seed=5)) == taken(DenseLayer(20, 8, 8, "cpu", seed=5))     # and can be had again
+
+
+def test_layers_begin_with_weights_of_their_own(calls):
+    a, b = DenseLayer(20, 8, 8, "cpu"), DenseLayer(20, 8, 8, "cpu")
+    assert not torch.equal(a.weight, b.weight)
+    assert torch.equal(DenseLayer(20, 8, 8, "cpu", seed=5).weight, DenseLayer(20, 8, 8, "cpu", seed=5).weight)
