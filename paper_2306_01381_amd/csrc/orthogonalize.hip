@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kBlock) void update_split_kernel(const T *g, int64_
         float v[kEach];
 #pragma unroll
         for (int k = 0; k < kEach; ++k) v[k] = (float)g[min(row, n_rows - 1) * ldg + min(col + k, n_cols - 1)];
-        if (at == blockIdx.x) scale = ldexp(1.0 / (sqrt(norm_square(partial + blockIdx.y * n_partial, n_partial, lds)) + eps), power);
+        if (at == blockIdx.x) scale = ldexp(one_over_norm(norm_square(partial + blockIdx.y * n_partial, n_partial, lds), eps), power);
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
             v[k] = row < n_rows && col + k < n_cols ? (float)((double)v[k] * scale) : 0.0f;      // behind the edge also where the scale is not finite
@@ -542,8 +542,7 @@ __global__ __launch_bounds__(kBlock) void update_scale_kernel(const T *g, int64_
                                                               int n_partial, double eps, T *out, int64_t ldo, int64_t stride_o, int64_t written)
 {
     __shared__ double lds[kWavesPerBlock];
-    const double total = norm_square(partial + blockIdx.y * n_partial, n_partial, lds);
-    const double scale = 1.0 / (sqrt(total) + eps);
+    const double scale = one_over_norm(norm_square(partial + blockIdx.y * n_partial, n_partial, lds), eps);
     g += blockIdx.y * stride;
     out += blockIdx.y * stride_o;
     for (int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x; at < n_rows * written; at += (int64_t)gridDim.x * kBlock) {

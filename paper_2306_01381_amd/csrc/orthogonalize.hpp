@@ -41,4 +41,8 @@ __device__ __forceinline__ double block_sum(double v, double *lds)
     return (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 
+// 1 / (norm + eps) of a matrix with this sum of squares.  fp32 elements that are finite keep the sum finite in 64 bits; one that is not makes the whole matrix NaN, where 1 / inf
+// would make zeros of the others.
+__device__ __forceinline__ double one_over_norm(double sum, double eps) { return __builtin_isfinite(sum) ? 1.0 / (sqrt(sum) + eps) : __builtin_nan(""); }
+
 }  // namespace adaqp

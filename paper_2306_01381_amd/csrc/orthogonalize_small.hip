@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void small_update_kernel(SmallUpdate u, i
     sum = 0.0;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) sum += squares[w];
-    const double scale = ldexp(1.0 / (sqrt(sum) + u.eps), u.power);
+    const double scale = ldexp(one_over_norm(sum, u.eps), u.power);
     const int n_there = flip ? u.n_cols : u.n_rows, m_there = flip ? u.n_rows : u.n_cols;
     for (int i = wave; i < kN; i += kWaves) {
         constexpr int kMost = kOwn * kWaves * 32 / kWave;

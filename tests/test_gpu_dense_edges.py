@@ -1,0 +1,44 @@
+"""The dense operators at the ends of their ranges: what is not finite, the largest magnitudes."""
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import dense as D                                        # noqa: E402
+from paper_2306_01381_amd import binding as B                      # noqa: E402
+
+DEV = "cuda:0"
+STEPS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+def _say(*what):
+    print(*what, flush=True)
+    sys.stdout.flush()
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+@pytest.mark.parametrize("rows,cols", [(50, 80), (33, 7), (200, 130), (700, 650)])
+def test_orthogonalize_of_what_is_not_finite(rows, cols, steps, bad, kind):
+    """One bad element makes its matrix NaN throughout, with and without steps, in every form; its neighbours keep their values."""
+    _say("orthogonalize not finite", rows, cols, steps, bad, kind)
+    gen = torch.Generator(device=DEV).manual_seed(rows)
+    g = torch.randn(3, rows, cols, generator=gen, device=DEV).to(kind)
+    work = torch.empty(max(1, B.adaqp_orthogonalize_workspace_bytes(3, rows, cols)), dtype=torch.uint8, device=DEV)
+    want, got = torch.empty_like(g), torch.empty_like(g)
+    B.adaqp_orthogonalize(g, want, STEPS[:steps], 1e-7, work)
+    g[1, rows // 2, cols - 1] = bad
+    B.adaqp_orthogonalize(g, got, STEPS[:steps], 1e-7, work)
+    assert bool(got[1].isnan().all())
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2]) and bool(want.isfinite().all())
