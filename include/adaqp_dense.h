@@ -78,10 +78,12 @@ int64_t adaqp_mx4_scale_bytes(int64_t n_rows, int64_t n_cols);
 /* Writes a matrix (x_dev [n_rows, ld] of `type`) as an MX matrix and / or its transpose as one, in one pass over x.
  * Per block (32 values of a row; for the transpose 32 values of a column; values beyond the edge count as zeros), m = the largest magnitude:
  *   NEAREST      e = floor(log2 m) - 2; each value / 2^e to the nearest of the code's values, ties to the even code, beyond 6 to 6
- *   STOCHASTIC   e = the smallest with m <= 6 * 2^e, so that nothing is clipped and the expected value is the value itself; with lo <= v / 2^e < hi the
+ *   STOCHASTIC   e = the smallest with m <= 6 * 2^e, so that nothing is clipped and the expected value is the value itself but for the 16 bits of
+ *                t, which take off less than 2^-16 of hi - lo; with lo <= v / 2^e < hi the
  *                neighbours among the code's values and t = trunc(2^16 * (v / 2^e - lo) / (hi - lo)), hi is taken where t + r >= 2^16 (magnitudes; the sign
  *                stays).  r = r16(seed, row, column) of the MX matrix that is written, Philox4x32-10 as in adaqp_quantize_pack with the last
- *                counter word 0x4d583443; for the transpose seed + 1.
+ *                counter word 0x4d583443; for the transpose seed + 1.  With e = 126 (m beyond 1.5 * 2^127) 3 stands in the place of 4: 2^128 is no
+ *                fp32 number.
  * e is at least -127.  A block with an infinity or NaN: scale byte 255, codes 0.
  *   codes_dev, scales_dev       the matrix; both NULL: not wanted
  *   codes_t_dev, scales_t_dev   its transpose (n_cols rows, n_rows columns); both NULL: not wanted
@@ -89,7 +91,7 @@ int64_t adaqp_mx4_scale_bytes(int64_t n_rows, int64_t n_cols);
 int adaqp_mx4_quantize(const void *x_dev, int64_t ld, int64_t n_rows, int64_t n_cols, int32_t type, int32_t rounding, uint64_t seed,
                        uint8_t *codes_dev, uint8_t *scales_dev, uint8_t *codes_t_dev, uint8_t *scales_t_dev, void *stream);
 
-/* The values of an MX matrix: x_dev [n_rows, ld] of `type`, written.  All are exact.
+/* The values of an MX matrix: x_dev [n_rows, ld] of `type`, written.  All are exact; those from 2^128 on, which adaqp_mx4_quantize writes none of, are infinite.
  * Errors: EINVAL, ESIZE, EHIP. */
 int adaqp_mx4_dequantize(const uint8_t *codes_dev, const uint8_t *scales_dev, int64_t n_rows, int64_t n_cols,
                          void *x_dev, int64_t ld, int32_t type, void *stream);

@@ -66,6 +66,7 @@ def mx4_quantize(x, seed=None):
         share = np.where(gap > 0, (y - VALUES[below]) / np.where(gap > 0, gap, 1.0), 0.0)
         r = philox16(rows, full.shape[1], seed).reshape(y.shape)
         code = np.where(np.floor(share * 65536) + r >= 65536, above, below)
+        code = np.where((e[:, :, None] == 126) & (code == 6), 5, code)         # 4 * 2^126 is no fp32 number
     code = np.where(bad[:, :, None], 0, code | (np.signbit(block).astype(np.int64) << 3)).reshape(rows, -1)
     codes = (code[:, 0::2] | code[:, 1::2] << 4).astype(np.uint8)
     byte = np.where(bad, 255, e + 127).astype(np.uint8)

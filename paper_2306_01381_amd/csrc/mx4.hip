@@ -14,6 +14,7 @@ namespace adaqp {
 namespace {
 
 constexpr uint32_t kMxTag = 0x4d583443u;
+constexpr uint32_t kLargestByte = 126 + 127;        // of magnitudes beyond 1.5 * 2^127, to be rounded stochastically
 constexpr int kLanes = kMxChunk / 8;                // of a row
 constexpr int kPassRows = kBlock / kLanes;          // a lane has one row of each pass
 
@@ -65,6 +66,10 @@ __device__ __forceinline__ uint32_t stochastic_codes(const float (&x)[8], uint32
     for (int j = 0; j < 8; ++j) {
         const uint32_t r = j % 2 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
         codes |= ((__builtin_bit_cast(uint32_t, __builtin_amdgcn_ldexpf(fabsf(x[j]), power)) + (r << 6)) >> 22) << (4 * j);
+    }
+    if (byte == kLargestByte) {                     // no fp32 number is 4 * 2^126: of magnitudes there (up to 4 units) code 6 becomes 5
+        const uint32_t six = codes >> 2 & codes >> 1 & 0x11111111u;
+        codes -= six;
     }
     return byte == 255 ? 0 : (codes & 0x77777777u) | (signs & 0x88888888u);
 }

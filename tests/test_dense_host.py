@@ -163,3 +163,20 @@ def test_wrappers_refuse_tensors_that_are_not_what_they_name():
         B.adaqp_orthogonalize(x, x, STEPS, 1e-7, None)
     with pytest.raises(ValueError):
         B._same("call", (3, 0), (4, 0))
+
+
+def test_stochastic_definition_holds_what_fp32_has():
+    """2^128 = 4 * 2^126 is never written; below, magnitudes of such a block are rounded as in any other."""
+    x = np.full((1, 32), 2.0 ** 128 * (1 - 2.0 ** -24))
+    x[0, 1:4] = [-x[0, 0], 1.25 * 2.0 ** 126, 0.5 * 2.0 ** 126]
+    seen = set()
+    for seed in range(64):
+        codes, scales = D.mx4_quantize(x, seed)
+        assert scales.ravel().tolist() == [253, 0, 0, 0]
+        v = D.mx4_values(codes, scales, 32)[0]
+        assert v[0] == 3 * 2.0 ** 126 == -v[1] and np.all(v[4:] == v[0]) and v[3] == 0.5 * 2.0 ** 126
+        seen.add(v[2] / 2.0 ** 126)
+    assert seen == {1.0, 1.5}
+    y = np.full((1, 32), 1.5 * 2.0 ** 127)                                    # the largest that the scale below holds
+    codes, scales = D.mx4_quantize(y, 3)
+    assert scales.ravel()[0] == 252 and np.array_equal(D.mx4_values(codes, scales, 32), y)

@@ -42,3 +42,27 @@ def test_orthogonalize_of_what_is_not_finite(rows, cols, steps, bad, kind):
     B.adaqp_orthogonalize(g, got, STEPS[:steps], 1e-7, work)
     assert bool(got[1].isnan().all())
     assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2]) and bool(want.isfinite().all())
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols", [(40, 200), (64, 64), (33, 31)])
+def test_stochastic_codes_of_the_largest_magnitudes_are_finite(rows, cols, kind):
+    """Beyond 1.5 * 2^127 the next of the codes' values may be 2^128, which fp32 does not have: 3 * 2^126 is taken.  Everything else as defined, by rows and by columns."""
+    _say("mx4 largest", rows, cols, kind)
+    rng = np.random.default_rng(cols)
+    x = rng.uniform(-1, 1, size=(rows, cols)) * rng.choice([2.0 ** 127.99, 2.0 ** 127, 2.0 ** 126, 2.0 ** 124], size=(rows, cols))
+    largest = float(torch.finfo(kind).max)
+    x[::3, ::5], x[1::7, 1::4] = largest, -largest
+    xd = torch.from_numpy(x).to(kind).clamp_(-largest, largest).to(DEV)
+    x = xd.double().cpu().numpy()
+    assert np.isfinite(x).all()
+    for seed in (1, 77, 2 ** 40 + 3):
+        packed, packed_t = B.mx4_empty(rows, cols, DEV), B.mx4_empty(cols, rows, DEV)
+        B.adaqp_mx4_quantize(xd, cols, B.MX4_STOCHASTIC, seed, packed, packed_t)
+        alone = B.mx4_empty(rows, cols, DEV)
+        B.adaqp_mx4_quantize(xd, cols, B.MX4_STOCHASTIC, seed, alone, None)
+        for got, want in ((packed, D.mx4_quantize(x, seed)), (packed_t, D.mx4_quantize(x.T, seed + 1)), (alone, D.mx4_quantize(x, seed))):
+            assert np.array_equal(got[0].cpu().numpy(), want[0]) and np.array_equal(got[1].cpu().numpy(), want[1])
+        back = torch.empty(rows, cols, dtype=kind, device=DEV)
+        B.adaqp_mx4_dequantize(packed, cols, back)
+        assert bool(back.isfinite().all()) and float(back.abs().max()) == 1.5 * 2.0 ** 127
