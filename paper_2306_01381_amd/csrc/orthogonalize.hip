@@ -579,7 +579,7 @@ int update_parts(int64_t n, int64_t lines, int64_t n_matrices)
 
 UpdateLayout update_layout(int32_t n_matrices, int64_t n_rows, int64_t n_cols)
 {
-    UpdateLayout u;
+    UpdateLayout u{};
     u.flip = n_rows > n_cols;
     u.n = padded(u.flip ? n_cols : n_rows);
     u.m = padded(u.flip ? n_rows : n_cols);
@@ -589,6 +589,10 @@ UpdateLayout update_layout(int32_t n_matrices, int64_t n_rows, int64_t n_cols)
     u.norm_blocks = n_rows * ((n_cols + kNormRun - 1) / kNormRun);
     if (u.norm_blocks > kNormBlocks) u.norm_blocks = kNormBlocks;
     u.partial_at = 0;
+    if (small_update_fits(n_rows, n_cols)) {        // its steps are in the LDS; without steps only the norms' sums are needed
+        u.bytes = (int64_t)n_matrices * kNormBlocks * 8;
+        return u;
+    }
     u.x_at = (n_matrices * u.norm_blocks * 8 + 255) / 256 * 256;
     u.a_at = u.x_at + 4 * n_matrices * u.big;
     u.q_at = u.a_at + n_matrices * u.small;

@@ -180,3 +180,11 @@ def test_stochastic_definition_holds_what_fp32_has():
     y = np.full((1, 32), 1.5 * 2.0 ** 127)                                    # the largest that the scale below holds
     codes, scales = D.mx4_quantize(y, 3)
     assert scales.ravel()[0] == 252 and np.array_equal(D.mx4_values(codes, scales, 32), y)
+
+
+def test_workspace_of_updates_in_one_launch_is_that_of_their_norms():
+    """Matrices that fit a CU's LDS need no memory for their steps; without steps their norms' partial sums: at most 512 of 8 bytes each."""
+    for count, rows, cols in ((1000, 64, 64), (65535, 64, 64), (3, 41, 256), (7, 256, 41), (1, 1, 1)):
+        need = B.adaqp_orthogonalize_workspace_bytes(count, rows, cols)
+        assert need % 256 == 0 and 0 < need <= count * 512 * 8
+    assert B.adaqp_orthogonalize_workspace_bytes(1, 65, 65) > 4 * 65 * 65 * 4
