@@ -3,6 +3,7 @@
 
 #include "adaqp_dense.h"
 #include "common.hpp"
+#include "grid.hpp"
 
 namespace adaqp {
 
@@ -76,6 +77,16 @@ __device__ __forceinline__ float lane_sum(float v)
         v = __builtin_bit_cast(float, (uint32_t)w[0]) + __builtin_bit_cast(float, (uint32_t)w[1]);
     }
     return v;
+}
+
+// A kernel's workgroup among those of grid_of().
+__device__ __forceinline__ uint32_t workgroup() { return blockIdx.y * gridDim.x + blockIdx.x; }
+__device__ __forceinline__ uint32_t workgroups() { return gridDim.y * gridDim.x; }
+
+inline dim3 grid_of(int64_t workgroups, int32_t threads, uint32_t z = 1)
+{
+    const GridSize g = grid_size(workgroups, threads);
+    return dim3(g.x, g.y, z);
 }
 
 // Workgroups are dealt to the eight XCDs in turn: the place of a workgroup in a grid (a multiple of eight) such that neighbouring places share an XCD.

@@ -132,7 +132,7 @@ __global__ __launch_bounds__(kBlock) void mx4_quantize_rows_kernel(MxArgs a)
 {
     constexpr int kEach = 2, kBlocks = kBlock / 4;
     if (STOCHASTIC) round_toward_zero();            // nothing but the scaling rounds here
-    const uint64_t first = (uint64_t)xcd_neighbour(blockIdx.x, gridDim.x) * (kBlocks * kEach) + threadIdx.x / 4;
+    const uint64_t first = (uint64_t)xcd_neighbour(workgroup(), workgroups()) * (kBlocks * kEach) + threadIdx.x / 4;
     const int l = threadIdx.x % 4;
     int64_t row[kEach];
     uint32_t block[kEach];
@@ -174,7 +174,7 @@ __global__ __launch_bounds__(kBlock) void mx4_quantize_kernel(MxArgs a)
     if (STOCHASTIC) round_toward_zero();
     // an XCD gets neighbouring tiles, four tile rows together: their parts of the columns' lines meet in its L2
     constexpr uint32_t kGroup = 4;
-    const uint32_t at = xcd_neighbour(blockIdx.x, gridDim.x);
+    const uint32_t at = xcd_neighbour(workgroup(), workgroups());
     const uint32_t group = at / (kGroup * a.tiles_c), in_group = at % (kGroup * a.tiles_c);
     if (group * kGroup >= a.tiles_r) return;
     const uint32_t rows = min(kGroup, a.tiles_r - group * kGroup);
@@ -261,7 +261,7 @@ template <typename T, int VW, bool WHOLE>
 __global__ __launch_bounds__(kBlock) void mx4_dequantize_kernel(const uint8_t *codes, const uint8_t *scales, int64_t n_rows, int64_t n_cols, int64_t written,
                                                                 int64_t pitch, T *x, int64_t ld, int64_t granules)
 {
-    const uint64_t at = (uint64_t)blockIdx.x * kBlock + threadIdx.x;
+    const uint64_t at = (uint64_t)workgroup() * kBlock + threadIdx.x;
     const int64_t row = at >> 32 ? at / (uint64_t)granules : (uint32_t)at / (uint32_t)granules, g = at - row * granules;
     if (row >= n_rows) return;
     float v[8];
@@ -283,9 +283,9 @@ void launch_quantize(const MxArgs &a, int32_t rounding, int64_t blocks, hipStrea
 {
     auto go = [&](auto stochastic) {
         constexpr bool S = decltype(stochastic)::value;
-        if (!a.codes_t)   mx4_quantize_rows_kernel<T, VW, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
-        else if (a.codes) mx4_quantize_kernel<T, VW, true, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
-        else              mx4_quantize_kernel<T, VW, false, S><<<(uint32_t)blocks, kBlock, 0, st>>>(a);
+        if (!a.codes_t)   mx4_quantize_rows_kernel<T, VW, S><<<grid_of(blocks, kBlock), kBlock, 0, st>>>(a);
+        else if (a.codes) mx4_quantize_kernel<T, VW, true, S><<<grid_of(blocks, kBlock), kBlock, 0, st>>>(a);
+        else              mx4_quantize_kernel<T, VW, false, S><<<grid_of(blocks, kBlock), kBlock, 0, st>>>(a);
     };
     if (rounding == ADAQP_MX4_STOCHASTIC) go(std::true_type());
     else                                  go(std::false_type());
@@ -306,13 +306,12 @@ hipError_t launch_dequantize(const uint8_t *codes, const uint8_t *scales, int64_
     const bool whole = whole_lines(x, ld, sizeof(T));
     const int64_t line = 128 / sizeof(T), written = whole ? (n_cols + line - 1) / line * line : n_cols;
     const int64_t granules = (written + 7) / 8, blocks = (n_rows * granules + kBlock - 1) / kBlock;
-    if (blocks > 0x7FFFFFFF) return hipErrorInvalidConfiguration;
     constexpr int VW = 16 / sizeof(T);
     int vw = VW;
     while (vw > 1 && (!aligned_to(x, vw * sizeof(T)) || ld % vw != 0)) vw /= 2;
     auto go = [&](auto vw, auto lines) {
         mx4_dequantize_kernel<T, decltype(vw)::value, decltype(lines)::value>
-            <<<(uint32_t)blocks, kBlock, 0, st>>>(codes, scales, n_rows, n_cols, written, mx_pitch(n_cols), (T *)x, ld, granules);
+            <<<grid_of(blocks, kBlock), kBlock, 0, st>>>(codes, scales, n_rows, n_cols, written, mx_pitch(n_cols), (T *)x, ld, granules);
     };
     if (whole)              go(std::integral_constant<int, VW>(), std::true_type());
     else if (vw == VW)      go(std::integral_constant<int, VW>(), std::false_type());
@@ -350,7 +349,7 @@ extern "C" int adaqp_mx4_quantize(const void *x_dev, int64_t ld, int64_t n_rows,
     // the columns' form writes whole chunks of 128 rows: two tiles of 64
     const int64_t tiles_r = mx_chunks(n_rows) * 2, tiles_c = mx_chunks(n_cols), row_blocks = (n_cols + kMxBlock - 1) / kMxBlock;
     const int64_t blocks = ((codes_t_dev ? tiles_r * tiles_c : (n_rows * row_blocks + kBlock / 2 - 1) / (kBlock / 2)) + 7) / 8 * 8;
-    if (blocks > 0x7FFFFFFF) return ADAQP_ESIZE;
+    if (blocks > kMostWorkgroups) return ADAQP_ESIZE;
     const int64_t bytes = element_bytes(type);
     const int vw = whole_lines(x_dev, ld, bytes) ? (int)(16 / bytes) : vector_elements(x_dev, ld, n_cols, bytes);       // in its own lines a vector may pass the last column
     int bits = 0;
@@ -372,7 +371,7 @@ extern "C" int adaqp_mx4_dequantize(const uint8_t *codes_dev, const uint8_t *sca
     if (n_rows >= kMxMost || n_cols >= kMxMost) return ADAQP_ESIZE;
     if (n_rows == 0 || n_cols == 0) return ADAQP_OK;
     if (!valid_mx(codes_dev, scales_dev) || !x_dev || ld < n_cols || !aligned_to(x_dev, element_bytes(type))) return ADAQP_EINVAL;
-    if ((n_cols + 127) / 8 * n_rows / kBlock >= 0x7FFFFFFF) return ADAQP_ESIZE;
+    if ((n_cols + 127) / 8 * n_rows / kBlock >= kMostWorkgroups) return ADAQP_ESIZE;
     if (type == ADAQP_F32) ADAQP_HIP_TRY((launch_dequantize<float>(codes_dev, scales_dev, n_rows, n_cols, x_dev, ld, (hipStream_t)stream)));
     else                   ADAQP_HIP_TRY((launch_dequantize<__bf16>(codes_dev, scales_dev, n_rows, n_cols, x_dev, ld, (hipStream_t)stream)));
     return ADAQP_OK;

@@ -156,7 +156,7 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
     __shared__ Stage<BM, BN> stage[STAGES];
     static_assert(sizeof(stage) >= kWavesPerBlock * 32 * sheet_pitch(FN) * 4, "the sheets lie where the operands were");
     using Loads = StepLoads<BM, BN>;
-    const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
+    const TilePlace place = tile_place(workgroup(), workgroups(), (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
     if (place.part < 0) return;
     const int64_t split = place.part, row0 = place.row * BM, col0 = place.col * BN;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_halves_kernel(MulArgs g)
     __shared__ HalfStage<BM, BN> stage[STAGES];
     static_assert(sizeof(stage) >= kWavesPerBlock * 32 * sheet_pitch(FN) * 4, "the sheets lie where the operands were");
     using Loads = HalfLoads<BM, BN>;
-    const TilePlace place = tile_place(blockIdx.x, gridDim.x, (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
+    const TilePlace place = tile_place(workgroup(), workgroups(), (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
     if (place.part < 0) return;
     const int64_t row0 = place.row * BM, col0 = place.col * BN;
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
@@ -418,9 +418,9 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_rows_kernel(MulArgs
     constexpr int kLines = 2;                       // under way
     __shared__ float parts[kFewWaves][kFewRows * 32];
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, r = lane % 32, h = lane / 32;
-    const int64_t col0 = (int64_t)blockIdx.x * 32;
+    const int64_t col0 = (int64_t)workgroup() * 32;
     const int64_t row_a = min((int64_t)r, g.m - 1), row_b = min(col0 + r, g.n - 1);
-    const int64_t begin = blockIdx.y * g.steps_per_split, end = min(begin + g.steps_per_split, g.steps);
+    const int64_t begin = blockIdx.z * g.steps_per_split, end = min(begin + g.steps_per_split, g.steps);
     mx_sums sums;
 #pragma unroll
     for (int q = 0; q < 16; ++q) sums[q] = 0.0f;
@@ -465,7 +465,7 @@ __global__ __launch_bounds__(kFewWaves * kWave) void mx4_few_rows_kernel(MulArgs
         float sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) sum += parts[w][at];
-        if (col < g.written) ((T *)g.out)[(blockIdx.y * g.m + row) * g.ldo + col] = col < g.n ? (T)sum : (T)0.0f;
+        if (col < g.written) ((T *)g.out)[(blockIdx.z * g.m + row) * g.ldo + col] = col < g.n ? (T)sum : (T)0.0f;
     }
 }
 
@@ -543,9 +543,9 @@ MulShape mul_shape(int64_t m, int64_t n, int64_t k)
 template <typename T>
 void launch_tiles(const MulArgs &g, const MulShape &s, hipStream_t st)
 {
-    const uint32_t blocks = (uint32_t)tile_blocks(s.tiles_m * s.tiles_n, s.splits);
+    const dim3 blocks = grid_of(tile_blocks(s.tiles_m * s.tiles_n, s.splits), kBlock);
     switch (s.tile) {
-        case FEW_ROWS:         mx4_few_rows_kernel<T><<<dim3((uint32_t)((g.written + 31) / 32), (uint32_t)s.splits), kFewWaves * kWave, 0, st>>>(g); break;
+        case FEW_ROWS:         mx4_few_rows_kernel<T><<<grid_of((g.written + 31) / 32, kFewWaves * kWave, (uint32_t)s.splits), kFewWaves * kWave, 0, st>>>(g); break;
         case TILE_64_64:       mx4_matmul_kernel<T, 64, 64, 4><<<blocks, kBlock, 0, st>>>(g); break;
         case TILE_128_64:      mx4_matmul_kernel<T, 128, 64, 2><<<blocks, kBlock, 0, st>>>(g); break;
         case TILE_128_64_HALVES: mx4_matmul_halves_kernel<T, 128, 64, 4><<<blocks, kBlock, 0, st>>>(g); break;

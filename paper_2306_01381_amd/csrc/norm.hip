@@ -347,7 +347,7 @@ __global__ __launch_bounds__(1024) void layernorm_params_kernel(const float *par
     constexpr int kCols = 32, kSlices = 1024 / kCols;
     __shared__ float lds[kSlices][kCols];
     const int c = threadIdx.x % kCols, slice = threadIdx.x / kCols;
-    const int64_t col = (int64_t)blockIdx.x * kCols + c, width = 2 * (int64_t)dim;
+    const int64_t col = (int64_t)workgroup() * kCols + c, width = 2 * (int64_t)dim;
     float sum = 0.0f;
     if (col < width) {
 #pragma unroll 8
@@ -559,7 +559,7 @@ extern "C" int adaqp_layernorm_backward(const void *x_dev, int64_t ldx, const vo
     }
     if (dgamma_dev) {
         const int64_t blocks = (2 * (int64_t)dim + 31) / 32;
-        layernorm_params_kernel<<<(uint32_t)blocks, 1024, 0, (hipStream_t)stream>>>((const float *)workspace_dev, (int32_t)s.blocks, dim, dgamma_dev,
+        layernorm_params_kernel<<<grid_of(blocks, 1024), 1024, 0, (hipStream_t)stream>>>((const float *)workspace_dev, (int32_t)s.blocks, dim, dgamma_dev,
                                                                                     dbeta_dev);
         ADAQP_HIP_TRY(hipGetLastError());
     }
