@@ -165,12 +165,17 @@ __global__ __launch_bounds__(kBlock) void mx4_quantize_rows_kernel(MxArgs a)
     }
 }
 
+constexpr int kTileRows = 64;
+struct alignas(16) Tile { float v[kTileRows * kMxChunk]; };
+
 // The columns' form, and the rows'.
 template <typename T, int VW, bool ROWS, bool STOCHASTIC>
 __global__ __launch_bounds__(kBlock) void mx4_quantize_kernel(MxArgs a)
 {
-    constexpr int kRows = 64, kPasses = kRows / kPassRows;
-    __shared__ float tile[kRows * kMxChunk];
+    constexpr int kRows = kTileRows, kPasses = kRows / kPassRows;
+    __shared__ Tile tile_of;
+    static_assert(alignof(Tile) % alignof(float4) == 0, "written in vectors");
+    float *tile = tile_of.v;
     if (STOCHASTIC) round_toward_zero();
     // an XCD gets neighbouring tiles, four tile rows together: their parts of the columns' lines meet in its L2
     constexpr uint32_t kGroup = 4;

@@ -36,7 +36,7 @@ struct MulArgs {
 };
 
 template <int BM, int BN>
-struct Stage {
+struct alignas(32) Stage {
     uint8_t a[BM * kLine], b[BN * kLine];
     uint32_t scales[kStepChunks * (BM + BN)];       // [2][BM], then [2][BN]
 };
@@ -154,6 +154,7 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
 {
     constexpr int FM = BM / 64, FN = BN / 64;       // 32 x 32 parts of a wave
     __shared__ Stage<BM, BN> stage[STAGES];
+    static_assert(alignof(decltype(stage)) % alignof(vec_of<float, 16 / sizeof(T)>) == 0 && alignof(decltype(stage)) % alignof(int4) == 0, "operands and sheets are read in vectors");
     static_assert(sizeof(stage) >= kWavesPerBlock * 32 * sheet_pitch(FN) * 4, "the sheets lie where the operands were");
     using Loads = StepLoads<BM, BN>;
     const TilePlace place = tile_place(workgroup(), workgroups(), (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);
@@ -250,7 +251,7 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_kernel(MulArgs g)
 // in a quarter of a step if they were to arrive in the rest; of half a line four fit, and loads and reads of the LDS alike lie one by one between the products
 // (8192 x 8192 x 4096 fp32 181 us in lines, 176 with the loads spread, 171 with the reads spread).  Short rows have less of an empty half line.
 template <int BM, int BN>
-struct HalfStage {
+struct alignas(32) HalfStage {
     uint8_t a[BM * kLine / 2], b[BN * kLine / 2];
     uint32_t scales[BM + BN];
 };
@@ -306,6 +307,7 @@ __global__ __launch_bounds__(kBlock) void mx4_matmul_halves_kernel(MulArgs g)
 {
     constexpr int FM = BM / 64, FN = BN / 64;
     __shared__ HalfStage<BM, BN> stage[STAGES];
+    static_assert(alignof(decltype(stage)) % alignof(vec_of<float, 16 / sizeof(T)>) == 0 && alignof(decltype(stage)) % alignof(int4) == 0, "operands and sheets are read in vectors");
     static_assert(sizeof(stage) >= kWavesPerBlock * 32 * sheet_pitch(FN) * 4, "the sheets lie where the operands were");
     using Loads = HalfLoads<BM, BN>;
     const TilePlace place = tile_place(workgroup(), workgroups(), (uint32_t)g.tiles_m, (uint32_t)g.tiles_n, (uint32_t)g.splits);

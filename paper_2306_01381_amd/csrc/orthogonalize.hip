@@ -287,7 +287,8 @@ __device__ __forceinline__ bool product_tile(const ProductArgs &g, int64_t &tr, 
 
 // A wave's 32 x 32 sums on their way out, in the LDS.
 constexpr int kSheetPitch = 36;
-struct Sheet { float v[32 * kSheetPitch]; };
+struct alignas(16) Sheet { float v[32 * kSheetPitch]; };
+static_assert(alignof(Sheet) % alignof(float4) == 0, "read in vectors");
 
 // 16 neighbouring columns of a held row, from a multiple of 16 on.
 __device__ __forceinline__ void store_held(uint8_t *to, const float (&v)[16])
