@@ -152,6 +152,8 @@ __global__ __launch_bounds__(kThreads) void small_update_kernel(SmallUpdate u, i
         float v[kMost];
 #pragma unroll
         for (int k = 0; k < kMost; ++k) v[k] = k * kWave < m && i < n_there && k * kWave + lane < m_there ? *reinterpret_cast<const float *>(x + i * pitch + (k * kWave + lane) * 4) : 0.0f;
+        // the row is written over as another type: without this the compiler may move a lane's writes before another lane's reads
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int k = 0; k < kMost; ++k)
             if (k * kWave + lane < m) put_held(x, pitch, i, k * kWave + lane, i < n_there && k * kWave + lane < m_there ? (float)((double)v[k] * scale) : 0.0f);
