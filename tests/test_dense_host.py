@@ -188,3 +188,49 @@ def test_workspace_of_updates_in_one_launch_is_that_of_their_norms():
         need = B.adaqp_orthogonalize_workspace_bytes(count, rows, cols)
         assert need % 256 == 0 and 0 < need <= count * 512 * 8
     assert B.adaqp_orthogonalize_workspace_bytes(1, 65, 65) > 4 * 65 * 65 * 4
+
+
+def test_layernorm_definition_has_the_gradients_of_differences():
+    """Slopes of sum(dy * y) along random directions of x, gamma and beta.  Central differences of 1e-5 are off by 1e-10 of third derivatives (about 1 here) and by 1e-11 of the sum's size: 1e-7
+    leaves room for both."""
+    rng = np.random.default_rng(11)
+    for rows, dim in ((1, 2), (5, 12), (20, 37)):
+        x, dy, gamma, beta = 2 * rng.standard_normal((rows, dim)) + 0.5, rng.standard_normal((rows, dim)), rng.standard_normal(dim), rng.standard_normal(dim)
+        eps, t = 1e-2, 1e-5
+        _, mean, rstd = D.layernorm(x, gamma, beta, eps)
+        dx, dgamma, dbeta = D.layernorm_backward(x, dy, mean, rstd, gamma)
+
+        def loss(x, gamma, beta):
+            return (dy * D.layernorm(x, gamma, beta, eps)[0]).sum()
+        for _ in range(4):
+            vx, vg, vb = rng.standard_normal((rows, dim)), rng.standard_normal(dim), rng.standard_normal(dim)
+            slope = (loss(x + t * vx, gamma + t * vg, beta + t * vb) - loss(x - t * vx, gamma - t * vg, beta - t * vb)) / (2 * t)
+            parts = [dx * vx, dgamma * vg, dbeta * vb]
+            assert abs(sum(p.sum() for p in parts) - slope) <= 1e-7 * (1 + sum(np.abs(p).sum() for p in parts))
+
+
+def test_mx4_definition_is_a_search_of_the_grid():
+    """Of random blocks: the power of two by its inequality, and no value of the grid nearer than the one that the code stands for, at ties an even code."""
+    rng = np.random.default_rng(12)
+    x = rng.standard_normal((40, 96)) * np.exp2(rng.integers(-9, 10, size=(40, 3)).repeat(32, 1))
+    x[::4] = np.round(x[::4] * 4) / 4                                         # ties among them
+    x[5, 32:64] = 0.0
+    grid = [float(v) for v in D.VALUES]
+    codes, scales = D.mx4_quantize(x)
+    code = np.stack([codes & 15, codes >> 4], -1).reshape(40, -1)[:, :96]
+    exponent = scales.transpose(1, 0, 2).reshape(40, -1)[:, :3].astype(int) - 127
+    _, upper = D.mx4_quantize(x, seed=9)
+    upper = upper.transpose(1, 0, 2).reshape(40, -1)[:, :3].astype(int) - 127
+    for r in range(40):
+        for b in range(3):
+            block, e, s = x[r, 32 * b:32 * b + 32], exponent[r, b], upper[r, b]
+            most = max(abs(v) for v in block)
+            if most == 0.0:
+                assert e == s == -127
+                continue
+            assert 4.0 * 2.0 ** e <= most < 8.0 * 2.0 ** e
+            assert 6.0 * 2.0 ** (s - 1) < most <= 6.0 * 2.0 ** s
+            for v, c in zip(block, code[r, 32 * b:32 * b + 32]):
+                far = [abs(abs(v) / 2.0 ** e - g) for g in grid]
+                assert far[c % 8] == min(far) and (far.count(min(far)) == 1 or c % 2 == 0)
+                assert (c >= 8) == (np.signbit(v))
