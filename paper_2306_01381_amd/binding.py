@@ -918,6 +918,10 @@ def adaqp_probe_xcd_of_workgroup(n_workgroups: int, device="cuda:0",
 
 # ---- adaqp_dense.h -----------------------------------------------------------------------------------------------------------------------
 
+# What these calls write (y, dx, x, out) may be a view of a wider tensor, but one whose first element lies on a 128-byte line and whose rows are a multiple of 128 bytes apart
+# owns its lines: each row is written to the end of the line that its last column lies in, with zeros behind that column.  Columns of the wider tensor that lie there are
+# lost: of a line-aligned fp32 matrix m, m[:, :40] as an output also clears m[:, 40:64].  Pass a tensor of its own, or a view that ends with a line.
+
 _TYPES = {torch.float32: 0, torch.bfloat16: 1}
 
 
@@ -957,6 +961,7 @@ def _count(name: str, *args) -> int:
 
 def adaqp_layernorm_forward(x: torch.Tensor, dim: int, gamma: Optional[torch.Tensor], beta: Optional[torch.Tensor], eps: float, y: torch.Tensor,
                             stats: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """y: rows that are whole 128-byte lines are written to their last line's end, zeros behind column `dim`."""
     xp, rows, ldx, kind = _elements(x, dim, "x")
     yp, rows_y, ldy, kind_y = _elements(y, dim, "y")
     _same("adaqp_layernorm_forward", (rows, kind), (rows_y, kind_y))
@@ -971,6 +976,7 @@ def adaqp_layernorm_workspace_bytes(n_rows: int, dim: int) -> int:
 def adaqp_layernorm_backward(x: torch.Tensor, dy: torch.Tensor, dim: int, stats: torch.Tensor, gamma: Optional[torch.Tensor], dx: Optional[torch.Tensor],
                              dgamma: Optional[torch.Tensor], dbeta: Optional[torch.Tensor], workspace: Optional[torch.Tensor],
                              stream: Optional[torch.cuda.Stream] = None) -> None:
+    """dx: rows that are whole 128-byte lines are written to their last line's end, zeros behind column `dim`."""
     xp, rows, ldx, kind = _elements(x, dim, "x")
     dyp, rows_dy, lddy, kind_dy = _elements(dy, dim, "dy")
     dxp, rows_dx, lddx, kind_dx = (None, rows, 0, kind) if dx is None else _elements(dx, dim, "dx")
@@ -1016,6 +1022,7 @@ def adaqp_mx4_quantize(x: torch.Tensor, n_cols: int, rounding: int, seed: int, p
 
 
 def adaqp_mx4_dequantize(packed: Tuple[torch.Tensor, torch.Tensor], n_cols: int, x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """x: rows that are whole 128-byte lines are written to their last line's end, zeros behind column n_cols."""
     xp, rows, ld, kind = _elements(x, n_cols, "x")
     cp, sp, _ = _mx4(packed, rows, n_cols, "packed")
     _check(lib().adaqp_mx4_dequantize(cp, sp, rows, n_cols, xp, ld, kind, _stream(stream)), "adaqp_mx4_dequantize")
@@ -1027,7 +1034,7 @@ def adaqp_mx4_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def adaqp_mx4_matmul(a: Tuple[torch.Tensor, torch.Tensor], b: Tuple[torch.Tensor, torch.Tensor], k: int, out: torch.Tensor,
                      workspace: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
-    """out = a b^T for MX matrices of k columns."""
+    """out = a b^T for MX matrices of k columns.  out: rows that are whole 128-byte lines are written to their last line's end, zeros behind b's last row's column."""
     ac, asc, m = _mx4(a, None, k, "a")
     bc, bsc, n = _mx4(b, None, k, "b")
     op, rows, ldo, kind = _elements(out, n, "out")
@@ -1042,7 +1049,8 @@ def adaqp_orthogonalize_workspace_bytes(n_matrices: int, n_rows: int, n_cols: in
 
 def adaqp_orthogonalize(g: torch.Tensor, out: torch.Tensor, coefficients, eps: float, workspace: Optional[torch.Tensor],
                         stream: Optional[torch.cuda.Stream] = None) -> None:
-    """g, out: [rows, cols] or [matrices, rows, cols].  coefficients: (a, b, c) of each step."""
+    """g, out: [rows, cols] or [matrices, rows, cols].  coefficients: (a, b, c) of each step.  out: rows that are whole 128-byte lines are written to their last line's end,
+    zeros behind the last column."""
     g, out = (t.unsqueeze(0) if t.dim() == 2 else t for t in (g, out))
     for t, name in ((g, "g"), (out, "out")):
         if not t.is_cuda or t.dtype not in _TYPES or t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):

@@ -234,3 +234,17 @@ def test_mx4_definition_is_a_search_of_the_grid():
                 far = [abs(abs(v) / 2.0 ** e - g) for g in grid]
                 assert far[c % 8] == min(far) and (far.count(min(far)) == 1 or c % 2 == 0)
                 assert (c >= 8) == (np.signbit(v))
+
+
+def test_wrappers_say_that_whole_lines_are_written():
+    """Outputs may be views: each wrapper that writes a matrix says what becomes of the columns behind it."""
+    for name in ("adaqp_layernorm_forward", "adaqp_layernorm_backward", "adaqp_mx4_dequantize", "adaqp_mx4_matmul", "adaqp_orthogonalize"):
+        assert "128-byte lines" in getattr(B, name).__doc__, name
+
+
+def test_the_updates_steps_do_what_their_comment_says():
+    from paper_2306_01381_amd.dense import UPDATE_STEPS
+    s = np.linspace(0.01, 1.0, 200_001)
+    for a, b, c in UPDATE_STEPS:
+        s = a * s + b * s ** 3 + c * s ** 5
+    assert 0.68 <= s.min() < 0.69 and 1.13 < s.max() <= 1.14
