@@ -4,8 +4,10 @@
 // the blocks of all rows are dealt out in a row, so that no lane stands for columns that do not exist.  For the columns' form a workgroup takes a tile of 128
 // columns and 64 rows through the LDS once, and a lane takes 32 rows of one column.  x is read once whichever of the two forms is wanted.  To nearest, the
 // conversions are gfx950's own, two values an instruction, and all is bound by memory: 4 bytes read per element of fp32 and 0.53 written per form.
-// Stochastically about 17 vector instructions per element and form, 8 of them Philox, are as long at work as the memory.
-// Measured: 58 000 x 602 fp32 to nearest, rows' form, 35 us (159 MB, 4.5 TB/s); 196 000 x 256 fp32, both forms, stochastic, 66 us (254 MB, 3.8 TB/s);
+// Stochastically the vector instructions are as long at work as the memory: of each element and form 17 where both forms are made, 8 of them Philox, and 26 where only
+// the rows' are, whose 8 values at a time look for their row and its end.
+// Measured: 58 000 x 602 fp32 to nearest, rows' form, 35 us (159 MB, 4.5 TB/s), both forms, as a layer's forward pass in training makes them, 38 us (177 MB, 4.7 TB/s);
+// 196 000 x 256 fp32, both forms, stochastic, 67 us of unpadded rows (254 MB, 3.8 TB/s), 55 of padded ones; half of the LDS's cycles are conflicts of the lanes that write the tile.
 // 179 000 x 300 bf16, rows' form, stochastic, 43 us (143 MB, 3.3 TB/s), and read back 29 us (143 MB, 5.0 TB/s).
 #include "mx4.hpp"
 #include "philox.hpp"
@@ -360,7 +362,7 @@ extern "C" int adaqp_mx4_quantize(const void *x_dev, int64_t ld, int64_t n_rows,
     int bits = 0;
     while (((int64_t)1 << bits) < row_blocks) ++bits;
     const bool below = n_rows * row_blocks + kBlock < ((int64_t)1 << 31);
-    const uint64_t factor = (((uint64_t)1 << (31 + bits)) + row_blocks - 1) / row_blocks;      // at most 2^31 + 1
+    const uint64_t factor = (((uint64_t)1 << (31 + bits)) + row_blocks - 1) / row_blocks;      // below 2^32: row_blocks is above 2^(bits - 1)
     MxArgs a{x_dev, ld, n_rows, n_cols, (uint32_t)tiles_r, (uint32_t)tiles_c, (uint32_t)row_blocks, below ? (uint32_t)factor : 0, (uint32_t)(31 + bits),
              n_cols % kMxBlock == 0 ? 0 : n_cols % vw ? 1 : 2, seed, codes_dev, scales_dev, codes_t_dev, scales_t_dev, mx_pitch(n_cols),
              mx_pitch(n_rows)};

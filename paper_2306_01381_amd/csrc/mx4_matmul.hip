@@ -7,10 +7,11 @@
 // Where the tiles are few, k is split over workgroups; the parts' sums, fp32, are added in order by a second kernel.  With at most 32 rows nothing is used
 // twice but those: a workgroup takes 32 columns of out, its eight waves share the lines of k and read them into registers, as many at a time as they can.
 //
-// What bounds it: large products the power that the matrix cores draw.  On random codes they reach 6.1 PFLOP/s from registers alone (9.0 on zeros, at a higher clock);
-// 8192 x 8192 x 4096, fp32 out, 171 us, 3.2 PFLOP/s, of which a tile's loop takes three quarters (33 of 43 us), its first loads 3 and its
-// stores 7.  Shallow products the output: 58 000 x 256, k = 602, 20 us (79 MB, 3.9 TB/s).  Deep ones the operands: 256 x 300, k = 196 000, 30 us and 5 to
-// add up the parts (58 MB).  Few rows their waits: 5 x 8192, k = 4096 and bf16 out, 7 us (17.9 MB, 2.6 TB/s).
+// What bounds it: large products the waits of a tile that has a CU to itself.  8192 x 8192 x 4096, fp32 out, takes 171 to 190 us with the clock that a run finds (about 3 PFLOP/s).  Of a tile's
+// 43 us its loop takes 33, at 73 % of what the matrix cores reach on random codes from registers alone (6.1 PFLOP/s): a wave has a SIMD to itself and nothing to fill its waits with.
+// Its first loads take 3 and its stores 7, with the matrix cores idle.  Power is a fifth: zeros, which draw less, take 141 us (61 at their rate from registers, 9.0 PFLOP/s).
+// Shallow products the output: 58 000 x 256, k = 602, 20 us (79 MB, 3.9 TB/s).  Deep ones the operands: 256 x 300, k = 196 000, 29 us and 5 to add up the parts; of 54 MB each line is
+// loaded by the 4 or 5 tiles of 64 x 64 that need it.  Few rows their waits: 5 x 8192, k = 4096 and bf16 out, 7 us (17.9 MB, 2.7 TB/s).
 #include "lines.hpp"
 #include "mx4.hpp"
 

@@ -4,7 +4,8 @@
 // squares and result need no second pass over memory, and the variance is that of the centred values.  Rows of up to 64 lanes' vectors lie
 // within a wave (64 / LPR rows in one), longer ones take the 256 lanes of a workgroup; rows beyond the registers of those are walked in memory.
 // Both directions are bound by memory: 8 and 12 bytes for about 8 and 15 operations on an element of fp32.  Measured: 58 000 x 602 fp32 forward 47 us (280 MB,
-// 6.0 TB/s), 306 000 x 256 fp32 backward with the gradients of gamma and beta 172 and 5 us (942 MB, 5.4 TB/s); a copy of 1 GiB runs at 5.0 TB/s.
+// 6.0 TB/s), 306 000 x 256 fp32 backward with the gradients of gamma and beta 171 and 5 us (942 MB, 5.4 TB/s); a copy of 1 GiB runs at 5.2 TB/s.  bf16, 58 000 x 602, forward 28 us
+// (140 MB, 5.0 TB/s), backward 61 with both kernels (209 MB, 3.4 TB/s): a group of lanes waits for a row, reduces it and only then asks for its next.
 //
 // Rows of bf16 that begin anywhere are read and written in vectors all the same, aligned to two bytes: 40 000 x 1937 forward 74 us, with an element a
 // lane 170.  Their last vector ends with the row and begins inside the one before; what both have counts once in the sums.

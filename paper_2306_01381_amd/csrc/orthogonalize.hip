@@ -3,16 +3,16 @@
 // With n <= m a step is three products: A = X X^T (n x n over m), Q = a I + b A + c A A (n x n over n) and X <- Q X (n x m over n).  A and Q are symmetric,
 // so only the tiles on and below the diagonal are computed and each is stored twice.
 //
-// fp32 products run at a sixteenth of the fp16 rate on this machine, and fp16 has 11 bits.  Every matrix is therefore held as hi + lo, two
+// fp32 products run at a tenth of the fp16 rate on this machine (8192^3: 0.15 and 1.47 PFLOP/s), and fp16 has 11 bits.  Every matrix is therefore held as hi + lo, two
 // fp16 numbers with 22 bits together, in units of a power of two that keeps the entries below 2^14 (the host knows a bound on the singular values after
 // every step), and a product is hi hi + hi lo + lo hi, summed in fp32: what is left out is below 2^-22 of a term.  Memory holds lines of 128 bytes: 32 hi,
 // then the 32 lo of the same columns, which is what a step of the products' loop takes of a row.  Both X and its transpose are kept, since the loop
 // runs along rows of both operands.
 //
 // What bounds it: matrices of some hundred rows the chain of launches, each about 4 us from its start over one or two waits for memory to its end (3 of 256 x 256:
-// 17 launches, 70 us; one of 602 x 256 the same); large ones the matrix cores: one of 2048 x 4096 1036 us, 0.87 PFLOP/s counting three fp16 products each (a large
-// fp16 product reaches 1.46).  Its step's products run at 1.1 PFLOP/s (103 GFLOP in 96 us), X X^T in 63 us and 10 to join, A A in 35 and 12; of zeros, which draw less, it
-// takes 850.
+// 17 launches, 70 us; one of 602 x 256 the same); large ones the matrix cores: one of 2048 x 4096 1020 to 1070 us with the clock that a run finds, 0.86 PFLOP/s counting three fp16 products
+// each (a large fp16 product reaches 1.47).  Its step's products run at 1.1 PFLOP/s (103 GFLOP in 96 us), X X^T in 61 us and 10 to join, A A in 34 and 11, whose 136 tiles in three cuts are
+// 408 workgroups for 512 places; of zeros, which draw less, it takes 814.
 #include <math.h>
 
 #include "lines.hpp"
