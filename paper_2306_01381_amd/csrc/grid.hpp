@@ -5,8 +5,8 @@
 
 namespace adaqp {
 
-// A launch has fewer than 2^32 threads in each dimension.  Workgroups beyond that go on in the second: number y * x_count + x, some more than were asked for, which
-// a kernel has to do nothing in.  Numbers stay neighbours of their XCD's: x is a multiple of eight wherever there is a second row of them.
+// A launch has fewer than 2^32 threads in each dimension.  Workgroups beyond that go on in the second: workgroup (i, j) is number j * x + i.  The last row may have more of
+// them than were asked for; they have nothing to do.  x is a multiple of eight where there are several rows, so that a number modulo eight still says its XCD.
 struct GridSize { uint32_t x, y; };
 
 constexpr int64_t kMostWorkgroups = (int64_t)1 << 31;        // of a launch
