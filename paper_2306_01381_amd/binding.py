@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libadaqp.so (include/adaqp.h, include/adaqp_dense.h).  Argument marshalling only.
+"""Thin ctypes binding of libadaqp.so (include/adaqp.h, include/adaqp_dense.h, include/adaqp_train.h).  Argument marshalling only.
 
 Every function has the name of the C entry point it calls.  Tensors are torch tensors that already live
 where the C function expects them (device tensors for *_dev arguments, numpy arrays for the host-only
@@ -21,6 +21,7 @@ OK, EINVAL, EBITS, ESIZE, EHIP = 0, -1, -2, -3, -4
 SERIAL, ISOLATED, FREE, CHAIN = 0, 1, 2, 3
 FORWARD, BACKWARD = 0, 1
 MX4_NEAREST, MX4_STOCHASTIC = 0, 1
+F8_ROWS, F8_TILES = 0, 1
 
 _i64, _i32, _u64, _vp = ctypes.c_int64, ctypes.c_int32, ctypes.c_uint64, ctypes.c_void_p
 
@@ -177,6 +178,21 @@ _SIGNATURES = {
     "adaqp_mx4_matmul": (ctypes.c_int, [_vp, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _i32, _vp, _i64, _vp]),
     "adaqp_orthogonalize_workspace_bytes": (ctypes.c_int, [_i32, _i64, _i64, ctypes.POINTER(_i64)]),
     "adaqp_orthogonalize": (ctypes.c_int, [_vp, _i64, _i64, _vp, _i64, _i64, _i32, _i64, _i64, _i32, _i32, _vp, ctypes.c_float, _vp, _i64, _vp]),
+    "adaqp_embedding_forward": (ctypes.c_int, [_vp, _i64, _i64, _i32, _i32, _vp, _i64, ctypes.c_float, _vp, _i64, _i32, _vp]),
+    "adaqp_embedding_sort_workspace_bytes": (ctypes.c_int, [_i64, _i64, ctypes.POINTER(_i64)]),
+    "adaqp_embedding_sort": (ctypes.c_int, [_vp, _i64, _i64, _vp, _vp, _vp, _i64, _vp]),
+    "adaqp_embedding_backward_workspace_bytes": (ctypes.c_int, [_i64, _i32, ctypes.POINTER(_i64)]),
+    "adaqp_embedding_backward": (ctypes.c_int, [_vp, _i64, _i64, _i32, _i32, _vp, _vp, _i64, ctypes.c_float, _i32, _vp, _i64, _vp, _i64, _vp]),
+    "adaqp_dropout": (ctypes.c_int, [_vp, _i64, _vp, _i64, _i64, _i32, _i32, ctypes.c_double, _u64, _i64, _vp, _vp, _i64, _vp]),
+    "adaqp_f8_code_bytes": (_i64, [_i64, _i64]),
+    "adaqp_f8_scale_bytes": (_i64, [_i64, _i64]),
+    "adaqp_f8_quantize": (ctypes.c_int, [_vp, _i64, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp]),
+    "adaqp_f8_dequantize": (ctypes.c_int, [_vp, _vp, _i64, _i64, _vp, _i64, _i32, _vp]),
+    "adaqp_f8_matmul_workspace_bytes": (ctypes.c_int, [_i64, _i64, _i64, ctypes.POINTER(_i64)]),
+    "adaqp_f8_matmul": (ctypes.c_int, [_vp, _vp, _i64, _vp, _vp, _i64, _i64, _vp, _i64, _i32, _vp, _i64, _vp]),
+    "adaqp_logprob_workspace_bytes": (ctypes.c_int, [_i64, _i32, _i32, ctypes.POINTER(_i64)]),
+    "adaqp_logprob_forward": (ctypes.c_int, [_vp, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _i64, _vp]),
+    "adaqp_logprob_backward": (ctypes.c_int, [_vp, _i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, ctypes.c_float, _vp, _i64, _vp]),
 }
 EXPORTS = tuple(_SIGNATURES)
 
@@ -1064,3 +1080,179 @@ def adaqp_orthogonalize(g: torch.Tensor, out: torch.Tensor, coefficients, eps: f
         return ld, t.stride(0) if count > 1 else max(t.stride(0), rows * ld)
     _check(lib().adaqp_orthogonalize(g.data_ptr(), *strides(g), out.data_ptr(), *strides(out), count, rows, cols, _TYPES[g.dtype], coef.shape[0],
                                      coef.ctypes.data, eps, *_workspace(workspace), _stream(stream)), "adaqp_orthogonalize")
+
+
+# ---- adaqp_train.h -----------------------------------------------------------------------------------------------------------------------
+
+# What was said above of outputs whose rows are whole 128-byte lines holds for these calls too.
+
+
+def _place(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> Optional[int]:
+    """The stream's handle.  Raises where the tensors do not lie on its device (None: the current one)."""
+    device = torch.cuda.current_device() if stream is None else stream.device_index
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor lies on {t.device}, the call's stream on device {device}")
+    return (_current_raw_stream(device) if stream is None else stream.cuda_stream) or None
+
+
+def _ints(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+    p = _dev(t, torch.int32, name)
+    if t is not None and t.numel() < n:
+        raise ValueError(f"{name} has {t.numel()} elements, {n} are wanted")
+    return p
+
+
+def adaqp_embedding_forward(table: torch.Tensor, dim: int, ids: torch.Tensor, scale: float, out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out: rows that are whole 128-byte lines are written to their last line's end, zeros behind column `dim`."""
+    tp, entries, ldt, kind_t = _elements(table, dim, "table")
+    op, rows, ldo, kind = _elements(out, dim, "out")
+    if ids.numel() != rows:
+        raise ValueError(f"{ids.numel()} ids, out has {rows} rows")
+    ip = _ints(ids, rows, "ids")
+    st = _place(stream, table, ids, out)
+    _check(lib().adaqp_embedding_forward(tp, ldt, entries, dim, kind_t, ip, rows, scale, op, ldo, kind, st), "adaqp_embedding_forward")
+
+
+def adaqp_embedding_sort_workspace_bytes(n_ids: int, n_entries: int) -> int:
+    return _count("adaqp_embedding_sort_workspace_bytes", n_ids, n_entries)
+
+
+def adaqp_embedding_sort(ids: torch.Tensor, n_entries: int, sorted_ids: torch.Tensor, order: torch.Tensor, workspace: Optional[torch.Tensor],
+                         stream: Optional[torch.cuda.Stream] = None) -> None:
+    n = ids.numel()
+    ip, sp, op = _ints(ids, n, "ids"), _ints(sorted_ids, n, "sorted_ids"), _ints(order, n, "order")
+    wp, wn = _workspace(workspace)
+    st = _place(stream, ids, sorted_ids, order, workspace)
+    _check(lib().adaqp_embedding_sort(ip, n, n_entries, sp, op, wp, wn, st), "adaqp_embedding_sort")
+
+
+def adaqp_embedding_backward_workspace_bytes(n_ids: int, dim: int) -> int:
+    return _count("adaqp_embedding_backward_workspace_bytes", n_ids, dim)
+
+
+def adaqp_embedding_backward(dy: torch.Tensor, dim: int, sorted_ids: torch.Tensor, order: torch.Tensor, scale: float, accumulate: bool, dtable: torch.Tensor,
+                             workspace: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """dtable: rows that are whole 128-byte lines are written to their last line's end, zeros behind column `dim`; with `accumulate` only columns are."""
+    yp, rows, lddy, kind = _elements(dy, dim, "dy")
+    tp, entries, ldd, kind_t = _elements(dtable, dim, "dtable")
+    if kind_t != 0:
+        raise TypeError("dtable must be fp32")
+    sp, op = _ints(sorted_ids, rows, "sorted_ids"), _ints(order, rows, "order")
+    wp, wn = _workspace(workspace)
+    st = _place(stream, dy, sorted_ids, order, dtable, workspace)
+    _check(lib().adaqp_embedding_backward(yp, lddy, rows, dim, kind, sp, op, entries, scale, int(bool(accumulate)), tp, ldd, wp, wn, st), "adaqp_embedding_backward")
+
+
+def adaqp_dropout(x: torch.Tensor, dim: int, p: float, seed: int, y: torch.Tensor, add: Optional[torch.Tensor] = None, first_row: int = 0,
+                  counter: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """counter: one int64 in device memory, added to the seed when the call runs.  y: rows that are whole 128-byte lines are written to their last line's end, zeros behind
+    column `dim`."""
+    xp, rows, ldx, kind = _elements(x, dim, "x")
+    yp, rows_y, ldy, kind_y = _elements(y, dim, "y")
+    ap, rows_a, lda, kind_a = (None, rows, 0, kind) if add is None else _elements(add, dim, "add")
+    _same("adaqp_dropout", (rows, kind), (rows_y, kind_y), (rows_a, kind_a))
+    cp = _dev(counter, torch.int64, "counter")
+    if counter is not None and counter.numel() < 1:
+        raise ValueError("counter has no element")
+    st = _place(stream, x, y, add, counter)
+    _check(lib().adaqp_dropout(xp, ldx, ap, lda, rows, dim, kind, p, seed & (2**64 - 1), first_row, cp, yp, ldy, st), "adaqp_dropout")
+
+
+def adaqp_f8_code_bytes(n_rows: int, n_cols: int) -> int:
+    return int(lib().adaqp_f8_code_bytes(n_rows, n_cols))
+
+
+def adaqp_f8_scale_bytes(n_rows: int, n_cols: int) -> int:
+    return int(lib().adaqp_f8_scale_bytes(n_rows, n_cols))
+
+
+def f8_empty(n_rows: int, n_cols: int, device="cuda:0") -> Tuple[torch.Tensor, torch.Tensor]:
+    """Uninitialised codes [n_rows, 128 ceil(n_cols / 128)] and scales [ceil(n_cols / 128), 16 ceil(n_rows / 16)] of an 8-bit matrix."""
+    chunks = -(-n_cols // 128)
+    return (torch.empty(n_rows, 128 * chunks, dtype=torch.uint8, device=device), torch.empty(chunks, -(-n_rows // 16) * 16, dtype=torch.uint8, device=device))
+
+
+def _f8(packed: Optional[Tuple[torch.Tensor, torch.Tensor]], n_rows: Optional[int], n_cols: int, name: str):
+    """(codes pointer, scales pointer, rows) of an 8-bit matrix of n_cols columns."""
+    if packed is None:
+        return None, None, n_rows
+    codes, scales = packed
+    rows = codes.shape[0] if n_rows is None else n_rows
+    cp, sp = _dev(codes, torch.uint8, f"{name} codes"), _dev(scales, torch.uint8, f"{name} scales")
+    chunks = -(-n_cols // 128)
+    if codes.shape != (rows, 128 * chunks) or scales.shape != (chunks, -(-rows // 16) * 16):
+        raise ValueError(f"{name}: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} are not those of {rows} rows and {n_cols} columns")
+    return cp, sp, rows
+
+
+def adaqp_f8_quantize(x: torch.Tensor, n_cols: int, blocks: int, packed: Optional[Tuple[torch.Tensor, torch.Tensor]],
+                      packed_t: Optional[Tuple[torch.Tensor, torch.Tensor]], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """packed, packed_t: (codes, scales) of the matrix and of its transpose, as f8_empty makes them."""
+    xp, rows, ld, kind = _elements(x, n_cols, "x")
+    cp, sp, _ = _f8(packed, rows, n_cols, "packed")
+    ctp, stp, _ = _f8(packed_t, n_cols, rows, "packed_t")
+    st = _place(stream, x, *(packed or ()), *(packed_t or ()))
+    _check(lib().adaqp_f8_quantize(xp, ld, rows, n_cols, kind, blocks, cp, sp, ctp, stp, st), "adaqp_f8_quantize")
+
+
+def adaqp_f8_dequantize(packed: Tuple[torch.Tensor, torch.Tensor], n_cols: int, x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """x: rows that are whole 128-byte lines are written to their last line's end, zeros behind column n_cols."""
+    xp, rows, ld, kind = _elements(x, n_cols, "x")
+    cp, sp, _ = _f8(packed, rows, n_cols, "packed")
+    st = _place(stream, x, *packed)
+    _check(lib().adaqp_f8_dequantize(cp, sp, rows, n_cols, xp, ld, kind, st), "adaqp_f8_dequantize")
+
+
+def adaqp_f8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
+    return _count("adaqp_f8_matmul_workspace_bytes", m, n, k)
+
+
+def adaqp_f8_matmul(a: Tuple[torch.Tensor, torch.Tensor], b: Tuple[torch.Tensor, torch.Tensor], k: int, out: torch.Tensor,
+                    workspace: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
+    """out = a b^T for 8-bit matrices of k columns.  out: rows that are whole 128-byte lines are written to their last line's end, zeros behind b's last row's column."""
+    ac, asc, m = _f8(a, None, k, "a")
+    bc, bsc, n = _f8(b, None, k, "b")
+    op, rows, ldo, kind = _elements(out, n, "out")
+    if rows != m:
+        raise ValueError(f"out has {rows} rows, a {m}")
+    wp, wn = _workspace(workspace)
+    st = _place(stream, *a, *b, out, workspace)
+    _check(lib().adaqp_f8_matmul(ac, asc, m, bc, bsc, n, k, op, ldo, kind, wp, wn, st), "adaqp_f8_matmul")
+
+
+def adaqp_logprob_workspace_bytes(n_rows: int, n_classes: int, n_top: int) -> int:
+    return _count("adaqp_logprob_workspace_bytes", n_rows, n_classes, n_top)
+
+
+def adaqp_logprob_forward(logits: torch.Tensor, n_classes: int, targets: Optional[torch.Tensor], logp: Optional[torch.Tensor], entropy: Optional[torch.Tensor] = None,
+                          stats: Optional[torch.Tensor] = None, top_logp: Optional[torch.Tensor] = None, top_class: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """top_logp, top_class: [rows, n_top], both or neither."""
+    xp, rows, ld, kind = _elements(logits, n_classes, "logits")
+    n_top = 0
+    for t, name in ((top_logp, "top_logp"), (top_class, "top_class")):
+        if t is not None:
+            if t.dim() != 2 or t.shape[0] != rows:
+                raise ValueError(f"{name} must have a row for each of {rows}")
+            n_top = max(n_top, t.shape[1])
+    tp = _ints(targets, rows, "targets")
+    lp, ep, sp = _vector(logp, rows, "logp"), _vector(entropy, rows, "entropy"), _vector(stats, 2 * rows, "stats")
+    vp, cp = _vector(top_logp, rows * n_top, "top_logp"), _ints(top_class, rows * n_top, "top_class")
+    wp, wn = _workspace(workspace)
+    st = _place(stream, logits, targets, logp, entropy, stats, top_logp, top_class, workspace)
+    _check(lib().adaqp_logprob_forward(xp, ld, rows, n_classes, kind, tp, lp, ep, sp, n_top, vp if n_top else None, cp if n_top else None, wp, wn, st), "adaqp_logprob_forward")
+
+
+def adaqp_logprob_backward(logits: torch.Tensor, n_classes: int, targets: Optional[torch.Tensor], stats: torch.Tensor, entropy: Optional[torch.Tensor],
+                           dlogp: Optional[torch.Tensor], dentropy: Optional[torch.Tensor], scale: float, dlogits: torch.Tensor,
+                           stream: Optional[torch.cuda.Stream] = None) -> None:
+    """dlogits: rows that are whole 128-byte lines are written to their last line's end, zeros behind column n_classes."""
+    xp, rows, ld, kind = _elements(logits, n_classes, "logits")
+    dp, rows_d, ldd, kind_d = _elements(dlogits, n_classes, "dlogits")
+    _same("adaqp_logprob_backward", (rows, kind), (rows_d, kind_d))
+    tp = _ints(targets, rows, "targets")
+    sp, ep = _vector(stats, 2 * rows, "stats"), _vector(entropy, rows, "entropy")
+    gp, hp = _vector(dlogp, rows, "dlogp"), _vector(dentropy, rows, "dentropy")
+    st = _place(stream, logits, targets, stats, entropy, dlogp, dentropy, dlogits)
+    _check(lib().adaqp_logprob_backward(xp, ld, rows, n_classes, kind, tp, sp, ep, gp, hp, scale, dp, ldd, st), "adaqp_logprob_backward")

@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libadaqp.so")
 SOURCES = ["codec.hip", "spmm.hip", "spmm_sliced.hip", "spmm_pieces.hip", "layer.hip", "assign.hip", "spmm_tiled.hip", "spmm_panels.hip",
            "spmm_blocks.hip", "probe.hip", "norm.hip", "mx4.hip", "mx4_matmul.hip", "orthogonalize.hip",
-           "orthogonalize_small.hip"]
+           "orthogonalize_small.hip", "embedding.hip", "dropout.hip", "f8.hip", "f8_matmul.hip", "logprob.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # -ffp-contract=off: the integer codes depend on every fp32 rounding, so nothing may be fused behind our back.
