@@ -45,47 +45,83 @@ __device__ __forceinline__ Part join(const Part &a, const Part &b)
     return Part{high.max != high.max || low.max != low.max ? __builtin_nanf("") : high.max, high.others + others, high.moment + moment};
 }
 
-// Adds N logits, not all of which are there (those are -inf).
-template <int N>
-__device__ __forceinline__ void add_logits(Part &p, const float (&x)[N])
-{
-    float most = x[0];
+// A lane's logits as they come: of the largest so far and the next, the smaller is counted and the larger kept, so that the largest of all is never counted.  Sums are in units of
+// exp(base), a logit that the lane has seen; it moves where they could grow out of fp32.  In powers of two, y = x log2(e) - base log2(e), one fma: what the rounding of its last term
+// does to all terms alike is taken back at the end (`off`).
+struct Running {
+    float base, shift, max, others, moment;         // shift = - base log2(e)
+
+    __device__ __forceinline__ void begin()
+    {
+        base = max = -__builtin_inff();
+        shift = others = moment = 0.0f;
+    }
+
+    // N logits, not all of which need be there (those are -inf); the largest of them.
+    template <int N>
+    __device__ __forceinline__ float add(const float (&x)[N])
+    {
+        float most = x[0];
 #pragma unroll
-    for (int k = 1; k < N; ++k) most = __builtin_elementwise_maximum(most, x[k]);          // NaN where there is one
-    if (most <= p.max) {
-        if (!is_part(p)) return;                    // all are -inf
+        for (int k = 1; k < N; ++k) most = __builtin_elementwise_maximum(most, x[k]);      // NaN where there is one
+        if (!(most <= base + 30.0f)) {              // the lane's first, NaN, or far above
+            const Part p = part();
+            base = most;
+            shift = -base * kLog2E;
+            others = moment = 0.0f;
+            if (is_part(p)) {
+                const float down = p.max - base, e = exp_of(down), clamped = fmaxf(down, kNothing) * kLog2E;
+                others = p.others * e;
+                moment = p.moment * kLog2E * e + clamped * others;
+            }
+        }
+        if (base == -__builtin_inff()) return most; // all are
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const float u = x[k] - p.max, e = exp_of(u);
-            p.others += e;
-            p.moment += fmaxf(u, kNothing) * e;
+            const float low = __builtin_elementwise_minimum(max, x[k]);
+            max = __builtin_elementwise_maximum(max, x[k]);
+            const float y = __builtin_elementwise_maximum(__builtin_fmaf(low, kLog2E, shift), kNothing * kLog2E), e = __builtin_amdgcn_exp2f(y);
+            others += e;
+            moment = __builtin_fmaf(y, e, moment);
         }
-        return;
+        return most;
     }
-    Part now{most, 0.0f, 0.0f};
-    bool one = true;                                // the largest that is not counted is still to come
-#pragma unroll
-    for (int k = 0; k < N; ++k) {
-        const float u = x[k] - most;
-        const bool is = one && x[k] == most;
-        const float e = is ? 0.0f : exp_of(u);
-        one = one && !is;
-        now.others += e;
-        now.moment += fmaxf(u, kNothing) * e;
+
+    __device__ __forceinline__ Part part() const
+    {
+        if (max == -__builtin_inff()) return no_part();
+        const float off = (float)(-(double)base * (double)kLog2E - (double)shift);
+        const float down = base - max, e = exp_of(down), sum = others * (e * __builtin_amdgcn_exp2f(off));
+        return Part{max, sum, __builtin_fmaf(__builtin_fmaf(off, kLn2, fmaxf(down, kNothing)), sum, moment * kLn2 * (e * __builtin_amdgcn_exp2f(off)))};
     }
-    p = join(p, now);
+};
+
+// The largest over LANES neighbouring lanes, NaN where there is one, in all of them.
+template <int LANES>
+__device__ __forceinline__ float lane_most(float v)
+{
+    auto moved = [](float x, auto pattern) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int32_t, x), decltype(pattern)::value, 0xF, 0xF, false));
+    };
+    if constexpr (LANES >= 2) v = __builtin_elementwise_maximum(v, moved(v, std::integral_constant<int, 0xB1>()));     // quad_perm [1, 0, 3, 2]
+    if constexpr (LANES >= 4) v = __builtin_elementwise_maximum(v, moved(v, std::integral_constant<int, 0x4E>()));     // quad_perm [2, 3, 0, 1]
+    if constexpr (LANES >= 8) v = __builtin_elementwise_maximum(v, moved(v, std::integral_constant<int, 0x141>()));    // row_half_mirror
+    if constexpr (LANES >= 16) v = __builtin_elementwise_maximum(v, moved(v, std::integral_constant<int, 0x140>()));   // row_mirror
+    if constexpr (LANES >= 32) v = __builtin_elementwise_maximum(v, __shfl_xor(v, 16));
+    if constexpr (LANES >= 64) v = __builtin_elementwise_maximum(v, __shfl_xor(v, 32));
+    return v;
 }
 
 // Over the lanes of a wave, in all of them.
-__device__ __forceinline__ Part join_lanes(Part p)
+__device__ __forceinline__ Part join_lanes(const Part &p)
 {
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-        const Part other{__shfl_xor(p.max, d), __shfl_xor(p.others, d), __shfl_xor(p.moment, d)};
-        const bool upper = threadIdx.x & d;         // both lanes join the same two in the same order
-        p = upper ? join(other, p) : join(p, other);
-    }
-    return p;
+    const float max = lane_most<kWave>(p.max);
+    if (max == -__builtin_inff()) return no_part();
+    const uint64_t with = __ballot(p.max == max);
+    const bool left_out = with && (int)(threadIdx.x % kWave) == __builtin_ctzll(with);      // one largest is not counted
+    const float down = p.max - max, e = exp_of(down);
+    const float others = p.others * e + (left_out ? 0.0f : e);
+    return Part{max, lane_sum<kWave>(others), lane_sum<kWave>(__builtin_fmaf(fmaxf(down, kNothing), others, p.moment * e))};
 }
 
 // ---- the largest --------------------------------------------------------------------------------------------------------------------------
@@ -105,11 +141,11 @@ __device__ __forceinline__ float key_value(uint32_t key)
 }
 __device__ __forceinline__ Place place_of(float x, uint32_t index) { return (Place)value_key(x) << 32 | (uint32_t)~index; }
 
-constexpr int kList = 256, kListEach = kList / kWave;
+constexpr int kList = 256, kPadding = 8;
 
 // A wave's.
 struct Largest {
-    Place *list;
+    Place *list;                                    // kList + kPadding
     int count, n_top;
     Place least;                                    // what is not above it is not among the largest
 
@@ -121,47 +157,98 @@ struct Largest {
         least = 0;
     }
 
-    // The list's n_top largest, in descending order, at its beginning.
-    __device__ __forceinline__ void cut()
+    // The n_top largest of the first EACH * 64, in descending order, to the list's beginning.
+    template <int EACH>
+    __device__ __forceinline__ void rank()
     {
         const int lane = threadIdx.x % kWave;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        Place mine[kListEach];
-        int above[kListEach];
+        Place mine[EACH];
+        int above[EACH];
 #pragma unroll
-        for (int i = 0; i < kListEach; ++i) {
+        for (int i = 0; i < EACH; ++i) {
             mine[i] = i * kWave + lane < count ? list[i * kWave + lane] : 0;
             above[i] = 0;
         }
-        for (int j = 0; j < count; ++j) {
-            const Place other = list[j];
+        for (int j = 0; j < count; j += kPadding)
 #pragma unroll
-            for (int i = 0; i < kListEach; ++i) above[i] += other > mine[i] ? 1 : 0;
-        }
+            for (int k = 0; k < kPadding; ++k) {
+                const Place other = list[j + k];
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) above[i] += other > mine[i] ? 1 : 0;
+            }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-        for (int i = 0; i < kListEach; ++i)
-            if (i * kWave + lane < count && above[i] < n_top) list[above[i]] = mine[i];
+        for (int i = 0; i < EACH; ++i)
+            if (mine[i] != 0 && above[i] < n_top) list[above[i]] = mine[i];
+    }
+
+    // The list's n_top largest, in descending order, at its beginning.
+    __device__ __forceinline__ void cut()
+    {
+        if (threadIdx.x % kWave < kPadding) list[count + threadIdx.x % kWave] = 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (count <= kWave) rank<1>();
+        else                rank<kList / kWave>();
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         count = min(count, n_top);
         if (count == n_top) least = list[n_top - 1];
     }
 
-    // One place of each lane that has one.
-    __device__ __forceinline__ void add(Place place, bool has)
+    // Before the first are added: the n_top-th largest of the lanes' best is a bound, so that hardly more than n_top of them are added.
+    __device__ __forceinline__ void bound(Place best)
     {
-        has = has && place > least;
-        uint64_t with = __ballot(has);
-        if (!with) return;
-        if (count + __popcll(with) > kList) {
-            cut();
-            has = has && place > least;
-            with = __ballot(has);
-        }
+        const uint64_t with = __ballot(best != 0);
+        if (__popcll(with) < n_top) return;
+        if (best != 0) list[__popcll(with & (((uint64_t)1 << threadIdx.x % kWave) - 1))] = best;
+        count = __popcll(with);
+        cut();
+        least -= 1;                                 // itself is to be added
+        count = 0;
+    }
+
+    // One place of each lane that has one; there is room for them.
+    __device__ __forceinline__ void add(Place place)
+    {
+        const bool has = place > least;
+        const uint64_t with = __ballot(has);
         if (has) list[count + __popcll(with & (((uint64_t)1 << threadIdx.x % kWave) - 1))] = place;
         count += __popcll(with);
     }
+
+    __device__ __forceinline__ void make_room()
+    {
+        if (count + kWave > kList) cut();
+    }
+
+    // N places of each lane that has them; other(k) gives place k once more, for a loop that is not unrolled.
+    template <int N, typename F>
+    __device__ __forceinline__ void add_all(const Place (&place)[N], F other)
+    {
+        int more = 0;
+#pragma unroll
+        for (int k = 0; k < N; ++k) more += __popcll(__ballot(place[k] > least));
+        if (more == 0) return;
+        if (count + more <= kList) {
+#pragma unroll
+            for (int k = 0; k < N; ++k) add(place[k]);
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < N; ++k) {
+                make_room();
+                add(other(k));
+            }
+        }
+    }
 };
+
+template <int N>
+__device__ __forceinline__ Place best_of(const Place (&place)[N])
+{
+    Place best = place[0];
+#pragma unroll
+    for (int k = 1; k < N; ++k) best = place[k] > best ? place[k] : best;
+    return best;
+}
 
 // ---- forward ------------------------------------------------------------------------------------------------------------------------------
 
@@ -180,37 +267,53 @@ struct ProbArgs {
 template <typename T>
 __device__ __forceinline__ float one_logit(const ProbArgs &a, int64_t row, int32_t j) { return (float)((const T *)a.logits)[row * a.ld + j]; }
 
-// What a row's part and largest come to: by the first threads of those that hold them.
+// What a row's part comes to.
+struct Prob {
+    float max, rest, entropy;
+    bool none;
+    __device__ __forceinline__ float logp(float x) const { return none ? -__builtin_inff() : (x - max) - rest; }
+};
+
+__device__ __forceinline__ Prob prob_of(const Part &p)
+{
+    Prob r;
+    r.none = !is_part(p);
+    const bool bad = !(p.max < __builtin_inff());
+    r.max = p.max;
+    r.rest = bad ? __builtin_nanf("") : r.none ? 0.0f : log1pf(p.others);
+    r.entropy = r.none ? 0.0f : r.rest - p.moment / (1.0f + p.others);
+    return r;
+}
+
+// By the first threads of those that hold a row's largest.
 template <typename T>
 __device__ __forceinline__ void store_row(const ProbArgs &a, int64_t row, const Part &p, int thread, const Place *largest)
 {
-    const bool none = !is_part(p), bad = !(p.max < __builtin_inff()) && !none;
-    const float rest = bad ? __builtin_nanf("") : none ? 0.0f : log1pf(p.others);
+    const Prob prob = prob_of(p);
     if (thread == 0) {
         if (a.stats) {
             a.stats[row * 2] = p.max;
-            a.stats[row * 2 + 1] = rest;
+            a.stats[row * 2 + 1] = prob.rest;
         }
-        if (a.entropy) a.entropy[row] = rest - (bad ? rest : p.moment / (1.0f + p.others));
+        if (a.entropy) a.entropy[row] = prob.entropy;
         if (a.logp) {
             const int32_t t = a.targets[row];
-            float v = 0.0f;
-            if (t >= 0 && t < a.n_classes) v = none ? -__builtin_inff() : (one_logit<T>(a, row, t) - p.max) - rest;
-            a.logp[row] = v;
+            a.logp[row] = t >= 0 && t < a.n_classes ? prob.logp(one_logit<T>(a, row, t)) : 0.0f;
         }
     }
     if (thread < a.n_top) {
         const Place place = largest[thread];
         a.top_class[row * a.n_top + thread] = (int32_t)~(uint32_t)place;
-        a.top_logp[row * a.n_top + thread] = none ? -__builtin_inff() : (key_value((uint32_t)(place >> 32)) - p.max) - rest;
+        a.top_logp[row * a.n_top + thread] = prob.logp(key_value((uint32_t)(place >> 32)));
     }
 }
 
 // A part of a row by a workgroup of WAVES waves, each of which has a contiguous share.
-template <typename T, int WAVES>
+template <typename T, int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES * kWave) void logprob_kernel(ProbArgs a)
 {
-    __shared__ Place lists[WAVES][kList];
+    constexpr int kPieces = 2, kAtOnce = kPieces * kWave * 8;
+    __shared__ Place lists[TOP ? WAVES : 1][TOP ? kList + kPadding : 1];
     __shared__ Part parts[WAVES];
     __shared__ int counts[WAVES];
     const uint64_t at = workgroup();
@@ -219,67 +322,200 @@ __global__ __launch_bounds__(WAVES * kWave) void logprob_kernel(ProbArgs a)
     const int32_t split = (int32_t)(at - row * a.splits), first = split * a.per_split, last = (int32_t)min((int64_t)first + a.per_split, (int64_t)a.n_classes);
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int32_t share = ((last - first + WAVES - 1) / WAVES + 7) / 8 * 8, begin = min(first + wave * share, last), end = min(begin + share, last);
-    Part p = no_part();
+    Running running;
+    running.begin();
     Largest largest;
-    largest.begin(lists[wave], a.n_top);
-    for (int32_t col0 = begin; col0 < end; col0 += kWave * 8) {
-        const int32_t col = col0 + lane * 8;
-        float x[8];
-        if (col < end) load_piece<T, 8>((const T *)a.logits, row * a.ld + col, end - col, a.span, x);
+    largest.begin(lists[TOP ? wave : 0], a.n_top);
+    auto take = [&](int32_t col0, const float (&x)[kPieces * 8]) {
+        const float most = running.add<kPieces * 8>(x);
+        if constexpr (TOP) {
+            if (!__ballot(!(most < key_value((uint32_t)(largest.least >> 32))))) return;        // none reaches the list (NaN does)
+            auto number = [&](int k) { return col0 + (k / 8 * kWave + lane) * 8 + k % 8; };
+            Place place[kPieces * 8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = col + k < end ? x[k] : -__builtin_inff();
-        add_logits<8>(p, x);
-        if (a.n_top) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) largest.add(place_of(x[k], (uint32_t)(col + k)), col + k < end);
+            for (int k = 0; k < kPieces * 8; ++k) place[k] = number(k) < end ? place_of(x[k], (uint32_t)number(k)) : 0;
+            if (col0 == begin) largest.bound(best_of(place));
+            largest.add_all(place, [&](int k) { return number(k) < end ? place_of(one_logit<T>(a, row, number(k)), (uint32_t)number(k)) : 0; });
         }
+    };
+    // what is whole is on its way while what is before it is counted
+    typedef loose_of<T, 8> Raw;
+    Raw next[kPieces];
+    auto load = [&](int32_t col0) {
+        const T *from = (const T *)a.logits + row * a.ld + col0 + lane * 8;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) next[i] = *reinterpret_cast<const Raw *>(from + i * kWave * 8);
+    };
+    if (end - begin >= kAtOnce) load(begin);
+    for (int32_t col0 = begin; col0 < end; col0 += kAtOnce) {
+        float x[kPieces * 8];
+        if (end - col0 >= kAtOnce) {
+#pragma unroll
+            for (int k = 0; k < kPieces * 8; ++k) x[k] = (float)next[k / 8].v[k % 8];
+            if (end - col0 >= 2 * kAtOnce) load(col0 + kAtOnce);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int32_t col = col0 + (i * kWave + lane) * 8;
+                float v[8];
+                if (col < end) load_piece<T, 8>((const T *)a.logits, row * a.ld + col, end - col, a.span, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[i * 8 + k] = col + k < end ? v[k] : -__builtin_inff();
+            }
+        }
+        take(col0, x);
     }
-    p = join_lanes(p);
-    if (a.n_top) largest.cut();
+    Part p = join_lanes(running.part());
+    if (TOP) largest.cut();
     if (lane == 0) {
         parts[wave] = p;
         counts[wave] = largest.count;
     }
     __syncthreads();
     if (wave != 0) return;
-    p = parts[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) p = join(p, parts[w]);
-    if (a.n_top)
-        for (int w = 1; w < WAVES; ++w) {
-            const int n = counts[w];
-            largest.add(lane < n ? lists[w][lane] : 0, lane < n);
-        }
-    if (a.n_top) largest.cut();
+    p = join_lanes(lane < WAVES ? parts[lane] : no_part());
+    if (TOP) {
+        static_assert(WAVES * kMostTop <= kList, "the waves' lists have room");
+        for (int w = 1; w < WAVES; ++w) largest.add(lane < counts[w] ? lists[TOP ? w : 0][lane] : 0);
+        largest.cut();
+    }
     if (a.splits == 1) {
         store_row<T>(a, row, p, lane, lists[0]);
         return;
     }
     if (lane == 0) a.parts[row * a.splits + split] = p;
-    if (lane < a.n_top) a.places[(row * a.splits + split) * a.n_top + lane] = lane < largest.count ? lists[0][lane] : 0;
+    if (TOP && lane < a.n_top) a.places[(row * a.splits + split) * a.n_top + lane] = lane < largest.count ? lists[0][lane] : 0;
+}
+
+// Rows of at most 64 lanes' registers: LANES lanes have one, PIECES pieces of 8 logits each.
+template <int LANES>
+__device__ __forceinline__ Place lane_most(Place v)
+{
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) {
+        const Place other = (Place)(uint32_t)__shfl_xor((int)(v >> 32), d) << 32 | (uint32_t)__shfl_xor((int)(uint32_t)v, d);
+        v = other > v ? other : v;
+    }
+    return v;
+}
+
+template <typename T, int LANES, int PIECES, int EACH, bool TOP>
+__global__ __launch_bounds__(kBlock) void logprob_rows_kernel(ProbArgs a)
+{
+    constexpr int kRows = kBlock / LANES;
+    __shared__ Place lists[TOP && LANES == kWave ? kWavesPerBlock : 1][TOP && LANES == kWave ? kList + kPadding : 1];
+    const int lane = threadIdx.x % LANES;
+    const int64_t row0 = (int64_t)workgroup() * (kRows * EACH) + threadIdx.x / LANES;
+    float x[EACH][PIECES * 8];
+    int32_t target[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int64_t row = min(row0 + e * kRows, a.n_rows - 1);
+        target[e] = a.logp ? a.targets[row] : -1;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) {
+            const int32_t col = (p * LANES + lane) * 8;
+            float v[8];
+            if (col < a.n_classes) load_piece<T, 8>((const T *)a.logits, row * a.ld + col, a.n_classes - col, a.span, v);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[e][p * 8 + k] = col + k < a.n_classes ? v[k] : -__builtin_inff();
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        const int64_t row = row0 + e * kRows;
+        float most = x[e][0];
+#pragma unroll
+        for (int k = 1; k < PIECES * 8; ++k) most = __builtin_elementwise_maximum(most, x[e][k]);
+        most = lane_most<LANES>(most);
+        float others = 0.0f, moment = 0.0f, of_target = 0.0f;
+        int equal = 0;                              // logits that are the largest
+#pragma unroll
+        for (int k = 0; k < PIECES * 8; ++k) {
+            const float u = x[e][k] - most;
+            const bool is = x[e][k] == most;
+            const float v = is ? 0.0f : exp_of(u);
+            equal += is ? 1 : 0;
+            others += v;
+            moment += fmaxf(u, kNothing) * v;
+            of_target += (k / 8 * LANES + lane) * 8 + k % 8 == target[e] ? x[e][k] : 0.0f;
+        }
+        others = lane_sum<LANES>(others) + (lane_sum<LANES>((float)equal) - 1.0f);
+        moment = lane_sum<LANES>(moment);
+        of_target = lane_sum<LANES>(of_target);
+        const Prob prob = prob_of(Part{most, others, moment});
+        if (lane == 0 && row < a.n_rows) {
+            if (a.stats) {
+                a.stats[row * 2] = most;
+                a.stats[row * 2 + 1] = prob.rest;
+            }
+            if (a.entropy) a.entropy[row] = prob.entropy;
+            if (a.logp) a.logp[row] = target[e] >= 0 && target[e] < a.n_classes ? prob.logp(of_target) : 0.0f;
+        }
+        if constexpr (TOP && LANES == kWave) {
+            auto number = [&](int k) { return (k / 8 * LANES + lane) * 8 + k % 8; };
+            Place place[PIECES * 8];
+#pragma unroll
+            for (int k = 0; k < PIECES * 8; ++k) place[k] = number(k) < a.n_classes ? place_of(x[e][k], (uint32_t)number(k)) : 0;
+            Largest largest;
+            largest.begin(lists[threadIdx.x / kWave], a.n_top);
+            largest.bound(best_of(place));
+            const int64_t there = min(row, a.n_rows - 1);
+            largest.add_all(place, [&](int k) { return number(k) < a.n_classes ? place_of(one_logit<T>(a, there, number(k)), (uint32_t)number(k)) : 0; });
+            largest.cut();
+            if (lane < a.n_top && row < a.n_rows) {
+                const Place now = lists[threadIdx.x / kWave][lane];
+                a.top_class[row * a.n_top + lane] = (int32_t)~(uint32_t)now;
+                a.top_logp[row * a.n_top + lane] = prob.logp(key_value((uint32_t)(now >> 32)));
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        } else if constexpr (TOP) {
+            Place place[PIECES * 8], best = 0;
+#pragma unroll
+            for (int k = 0; k < PIECES * 8; ++k) {
+                const int32_t j = (k / 8 * LANES + lane) * 8 + k % 8;
+                place[k] = j < a.n_classes ? place_of(x[e][k], (uint32_t)j) : 0;
+                best = place[k] > best ? place[k] : best;
+            }
+            for (int n = 0; n < a.n_top; ++n) {
+                const Place now = lane_most<LANES>(best);
+                if (lane == n % LANES && row < a.n_rows) {
+                    a.top_class[row * a.n_top + n] = (int32_t)~(uint32_t)now;
+                    a.top_logp[row * a.n_top + n] = prob.logp(key_value((uint32_t)(now >> 32)));
+                }
+                if (best == now) {                  // this lane's: its next below
+                    best = 0;
+#pragma unroll
+                    for (int k = 0; k < PIECES * 8; ++k) best = place[k] < now && place[k] > best ? place[k] : best;
+                }
+            }
+        }
+    }
 }
 
 // The splits of a row, a wave.
 template <typename T>
 __global__ __launch_bounds__(kWave) void logprob_join_kernel(ProbArgs a)
 {
-    __shared__ Place list[kList];
+    constexpr int kAtOnce = 16;
+    __shared__ Place list[kList + kPadding];
     const int64_t row = workgroup();
     if (row >= a.n_rows) return;
     const int lane = threadIdx.x;
     Part p = no_part();
     for (int32_t s = lane; s < a.splits; s += kWave) p = join(p, a.parts[row * a.splits + s]);
-    p = join_lanes(p);
     Largest largest;
     largest.begin(list, a.n_top);
-    if (a.n_top) {
-        const int32_t n = a.splits * a.n_top;
-        for (int32_t i = 0; i < n; i += kWave) {
-            const Place place = i + lane < n ? a.places[row * n + i + lane] : 0;
-            largest.add(place, place != 0);
-        }
-        largest.cut();
+    const int32_t n = a.splits * a.n_top;
+    for (int32_t i = 0; i < n; i += kAtOnce * kWave) {
+        Place place[kAtOnce];
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) place[k] = i + k * kWave + lane < n ? a.places[row * n + i + k * kWave + lane] : 0;
+        if (i == 0) largest.bound(best_of(place));
+        largest.add_all(place, [&](int k) { return i + k * kWave + lane < n ? a.places[row * n + i + k * kWave + lane] : 0; });
     }
+    p = join_lanes(p);
+    if (a.n_top) largest.cut();
     store_row<T>(a, row, p, lane, list);
 }
 
@@ -303,11 +539,27 @@ ProbShape prob_shape(int64_t n_rows, int32_t n_classes, int32_t n_top)
     return s;
 }
 
+template <typename T, int LANES, int PIECES>
+void launch_rows(const ProbArgs &a, hipStream_t st)
+{
+    constexpr int kEach = PIECES == 1 ? 2 : 1, kRows = kBlock / LANES * kEach;
+    const dim3 grid = grid_of((a.n_rows + kRows - 1) / kRows, kBlock);
+    if (a.n_top) logprob_rows_kernel<T, LANES, PIECES, kEach, true><<<grid, kBlock, 0, st>>>(a);
+    else         logprob_rows_kernel<T, LANES, PIECES, kEach, false><<<grid, kBlock, 0, st>>>(a);
+}
+
 template <typename T>
 hipError_t launch_forward(const ProbArgs &a, hipStream_t st)
 {
-    if (a.n_classes <= 2048) logprob_kernel<T, 1><<<grid_of(a.n_rows * a.splits, kWave), kWave, 0, st>>>(a);
-    else                     logprob_kernel<T, 4><<<grid_of(a.n_rows * a.splits, kBlock), kBlock, 0, st>>>(a);
+    if (a.n_classes <= 32)       launch_rows<T, 4, 1>(a, st);
+    else if (a.n_classes <= 64)  launch_rows<T, 8, 1>(a, st);
+    else if (a.n_classes <= 128) launch_rows<T, 16, 1>(a, st);
+    else if (a.n_classes <= 256) launch_rows<T, 32, 1>(a, st);
+    else if (a.n_classes <= 512) launch_rows<T, 64, 1>(a, st);
+    else if (a.n_classes <= 1024) launch_rows<T, 64, 2>(a, st);
+    else if (a.n_classes <= 2048) launch_rows<T, 64, 4>(a, st);
+    else if (a.n_top)             logprob_kernel<T, 4, true><<<grid_of(a.n_rows * a.splits, kBlock), kBlock, 0, st>>>(a);
+    else                          logprob_kernel<T, 4, false><<<grid_of(a.n_rows * a.splits, kBlock), kBlock, 0, st>>>(a);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess || a.splits == 1) return err;
     logprob_join_kernel<T><<<grid_of(a.n_rows, kWave), kWave, 0, st>>>(a);
@@ -332,7 +584,8 @@ template <typename T>
 __global__ __launch_bounds__(kBlock) void logprob_gradient_kernel(ProbGradArgs a)
 {
     constexpr int kEach = 2;
-    const uint64_t first = (uint64_t)workgroup() * (kBlock * kEach) + threadIdx.x;
+    // from the last row to the first: what the forward pass read last may still lie in the caches
+    const uint64_t first = (uint64_t)(workgroups() - 1 - workgroup()) * (kBlock * kEach) + threadIdx.x;
     int64_t row[kEach];
     int32_t col[kEach];
     float x[kEach][8];
