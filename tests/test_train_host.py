@@ -37,7 +37,7 @@ def test_workspaces():
     for ids, entries in ((1, 0), (1, 1), (5000, 600), (1 << 20, 1 << 30), ((1 << 31) - 1, (1 << 31) - 1)):
         need = B.adaqp_embedding_sort_workspace_bytes(ids, entries)
         assert need > 0 and need % 256 == 0
-    assert B.adaqp_embedding_backward_workspace_bytes(0, 8) == B.adaqp_embedding_backward_workspace_bytes(32, 8) == 0
+    assert B.adaqp_embedding_backward_workspace_bytes(0, 8) == B.adaqp_embedding_backward_workspace_bytes(8, 8) == 0
     assert B.adaqp_embedding_backward_workspace_bytes(33, 8) % 256 == 0 and B.adaqp_embedding_backward_workspace_bytes(33, 8) >= 2 * 2 * 8 * 4
     assert B.adaqp_logprob_workspace_bytes(0, 8, 0) == B.adaqp_logprob_workspace_bytes(100_000, 41, 5) == 0
     assert B.adaqp_logprob_workspace_bytes(1, 128_000, 20) > 0 and B.adaqp_logprob_workspace_bytes(1, 128_000, 20) % 256 == 0
