@@ -1,7 +1,7 @@
 // Matrices in 8 bits: writing them from rows, columns or both, and reading them back (adaqp_train.h).
 //
 // 16 lanes hold the 128 columns of a block, 8 neighbouring ones each.  Where only the rows' form with a scale for each row is wanted the blocks of all rows are dealt out in a row; else a
-// workgroup takes a tile of 128 columns and 128 rows in registers, and through the LDS for the columns' form.  x is read once.
+// workgroup takes a tile of 128 columns and 128 rows in registers.  x is read once.
 #include "f8.hpp"
 #include "rows.hpp"
 
@@ -32,16 +32,25 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t most)
     return byte < 0 ? 0 : byte;
 }
 
+// The scale as the conversions take it: they go by its exponent, and 0 is 2^-127.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+typedef short two_codes __attribute__((ext_vector_type(2)));     // in its lower or upper half
+
 // The codes of 4 values.
 __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d, uint32_t byte)
 {
-    // times 2^-e: exact but where it is far below the smallest code
-    const float unit = __builtin_bit_cast(float, (254u - byte) << 23);
-    int word = 0;
-    word = __builtin_amdgcn_cvt_pk_fp8_f32(a * unit, b * unit, word, false);
-    word = __builtin_amdgcn_cvt_pk_fp8_f32(c * unit, d * unit, word, true);
-    if (byte == kLargestByte) word -= word >> 3 & word >> 4 & word >> 5 & word >> 6 & 0x01010101;      // 256 becomes 240
-    return byte == 255 ? 0 : (uint32_t)word;
+    two_codes v = {0, 0};
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, a, b, scale_of(byte), false);
+    v = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(v, c, d, scale_of(byte), true);
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// What conversions do not know: blocks that are NaN have codes 0, and 256 becomes 240 where it would be 2^128.
+__device__ __forceinline__ uint32_t kept_codes(uint32_t word, uint32_t byte)
+{
+    if (byte == kLargestByte) word -= word >> 3 & word >> 4 & word >> 5 & word >> 6 & 0x01010101;
+    return byte == 255 ? 0 : word;
 }
 
 __device__ __forceinline__ float largest(const float (&x)[8])
@@ -88,78 +97,120 @@ __global__ __launch_bounds__(kBlock) void f8_quantize_rows_kernel(F8Args a)
         const uint32_t byte = scale_byte(most_of_block(magnitude(largest(x[e]))));
         if (first + e * kBlocks >= a.blocks) continue;
         *reinterpret_cast<uint2 *>(a.codes + (row[e] * a.chunks + chunk[e]) * kF8Block + l * 8) =
-            make_uint2(codes_of(x[e][0], x[e][1], x[e][2], x[e][3], byte), codes_of(x[e][4], x[e][5], x[e][6], x[e][7], byte));
+            make_uint2(kept_codes(codes_of(x[e][0], x[e][1], x[e][2], x[e][3], byte), byte), kept_codes(codes_of(x[e][4], x[e][5], x[e][6], x[e][7], byte), byte));
         uint8_t *scales = a.scales + chunk[e] * a.scale_pitch;
         if (l == 0) scales[row[e]] = (uint8_t)byte;
         if (row[e] == a.n_rows - 1 && a.n_rows + l < a.scale_pitch) scales[a.n_rows + l] = 0;
     }
 }
 
-constexpr int kTile = kF8Block;
-constexpr int kPassRows = kBlock / 16, kPasses = kTile / kPassRows;
+constexpr int kTile = kF8Block, kTilePieces = kTile / 8;
 
-// A tile of 128 rows and 128 columns: the columns' form, the rows' form or both, a scale for each row or for the tile.
+// Over the four groups of 16 lanes.
+__device__ __forceinline__ uint32_t most_of_groups(uint32_t most)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(most, most, false, false);
+    most = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(most, most, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+
+// A tile of 128 rows and 128 columns, of which a thread has 8 x 8: the columns' form, the rows' form or both, a scale for each row (column) or for the tile.  A column's largest is found over
+// the threads that have it, its codes are made where the values are, and only they, a quarter of the bytes, pass the LDS.
 template <typename T, bool TILES>
 __global__ __launch_bounds__(kBlock) void f8_quantize_kernel(F8Args a)
 {
-    constexpr int kPitch = kTile + 4;
-    __shared__ float tile[kTile * kPitch];
-    __shared__ uint32_t most_of[kWavesPerBlock];
+    __shared__ uint2 turned[kTile * kTilePieces];   // codes of the transpose: of each column 16 pieces of 8 rows
+    __shared__ uint4 most_of_cols[kWavesPerBlock][kTile / 4];
+    __shared__ uint32_t most_of_tile[kWavesPerBlock];
     const uint64_t at = workgroup();
     const int64_t tile_r = at / a.tiles_c, tile_c = at % a.tiles_c;
     if (tile_r >= a.tiles_r) return;
-    const int l = threadIdx.x % 16, r = threadIdx.x / 16;
-    const int64_t col = tile_c * kTile + l * 8, row0 = tile_r * kTile;
-    const int left = (int)min(a.n_cols - col, (int64_t)8);
-    float x[kPasses][8];
+    const int l = threadIdx.x % kTilePieces, r = threadIdx.x / kTilePieces, wave = threadIdx.x / kWave;    // columns 8 l .., rows 8 r ..
+    const int64_t col = tile_c * kTile + l * 8, row0 = tile_r * kTile + r * 8;
+    const int left = (int)min(max(a.n_cols - col, (int64_t)0), (int64_t)8);
+    float x[8][8];
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int64_t row = row0 + p * kPassRows + r;
-        const bool there = row < a.n_rows && left > 0;
-        if (there) load_piece<T, 8>((const T *)a.x, row * a.ld + col, left, a.span, x[p]);
+    for (int p = 0; p < 8; ++p) {
+        const bool there = row0 + p < a.n_rows && left > 0;
+        if (there) load_piece<T, 8>((const T *)a.x, (row0 + p) * a.ld + col, left, a.span, x[p]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) x[p][k] = there && k < left ? x[p][k] : 0.0f;
     }
-    uint32_t byte_of_tile = 0;
+    uint32_t tile_byte = 0;
     if (TILES) {
         uint32_t most = 0;
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) most = max(most, magnitude(largest(x[p])));
-#pragma unroll
-        for (int d = 1; d < kWave; d *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, d));
-        if (threadIdx.x % kWave == 0) most_of[threadIdx.x / kWave] = most;
+        for (int p = 0; p < 8; ++p) most = max(most, magnitude(largest(x[p])));
+        most = most_of_groups(most_of_block(most));
+        if (threadIdx.x % kWave == 0) most_of_tile[wave] = most;
         __syncthreads();
-        byte_of_tile = scale_byte(max(max(most_of[0], most_of[1]), max(most_of[2], most_of[3])));
+        tile_byte = scale_byte(max(max(most_of_tile[0], most_of_tile[1]), max(most_of_tile[2], most_of_tile[3])));
     }
     if (a.codes) {
+        uint32_t bytes[2] = {0, 0};
 #pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-            const int64_t row = row0 + p * kPassRows + r;
-            const uint32_t byte = TILES ? byte_of_tile : scale_byte(most_of_block(magnitude(largest(x[p]))));
-            if (row < a.n_rows)
-                *reinterpret_cast<uint2 *>(a.codes + (row * a.chunks + tile_c) * kF8Block + l * 8) =
-                    make_uint2(codes_of(x[p][0], x[p][1], x[p][2], x[p][3], byte), codes_of(x[p][4], x[p][5], x[p][6], x[p][7], byte));
-            if (l == 0 && row < a.scale_pitch) a.scales[tile_c * a.scale_pitch + row] = row < a.n_rows ? (uint8_t)byte : 0;
+        for (int p = 0; p < 8; ++p) {
+            const uint32_t byte = TILES ? tile_byte : scale_byte(most_of_block(magnitude(largest(x[p]))));
+            const bool there = row0 + p < a.n_rows;
+            if (there)
+                *reinterpret_cast<uint2 *>(a.codes + ((row0 + p) * a.chunks + tile_c) * kF8Block + l * 8) =
+                    make_uint2(kept_codes(codes_of(x[p][0], x[p][1], x[p][2], x[p][3], byte), byte), kept_codes(codes_of(x[p][4], x[p][5], x[p][6], x[p][7], byte), byte));
+            bytes[p / 4] |= (there ? byte : 0) << (8 * (p % 4));
         }
+        if (l == 0 && row0 < a.scale_pitch) *reinterpret_cast<uint2 *>(a.scales + tile_c * a.scale_pitch + row0) = make_uint2(bytes[0], bytes[1]);
     }
     if (!a.codes_t) return;
+    uint32_t byte_of[8];
+    if (TILES) {
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p)
+        for (int k = 0; k < 8; ++k) byte_of[k] = tile_byte;
+    } else {
+        uint32_t most[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) tile[(l * 8 + k) * kPitch + p * kPassRows + r] = x[p][k];  // transposed
+        for (int k = 0; k < 8; ++k) {
+            float v[8];
+#pragma unroll
+            for (int p = 0; p < 8; ++p) v[p] = x[p][k];
+            most[k] = most_of_groups(magnitude(largest(v)));
+        }
+        if (threadIdx.x % kWave < kTilePieces) {
+            most_of_cols[wave][l * 2] = make_uint4(most[0], most[1], most[2], most[3]);
+            most_of_cols[wave][l * 2 + 1] = make_uint4(most[4], most[5], most[6], most[7]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWavesPerBlock; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint4 m = most_of_cols[w][l * 2 + h];
+                most[h * 4] = max(most[h * 4], m.x);
+                most[h * 4 + 1] = max(most[h * 4 + 1], m.y);
+                most[h * 4 + 2] = max(most[h * 4 + 2], m.z);
+                most[h * 4 + 3] = max(most[h * 4 + 3], m.w);
+            }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) byte_of[k] = scale_byte(most[k]);
+    }
+    // of column 8 l + k the piece of rows 8 r .. is at place r ^ l of line 8 l + (k ^ l mod 2): the lanes of a wave that write the same k share all banks evenly
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        turned[(l * 8 + (k ^ l % 2)) * kTilePieces + (r ^ l)] =
+            make_uint2(kept_codes(codes_of(x[0][k], x[1][k], x[2][k], x[3][k], byte_of[k]), byte_of[k]), kept_codes(codes_of(x[4][k], x[5][k], x[6][k], x[7][k], byte_of[k]), byte_of[k]));
+    if (r == 0 && col < a.scale_pitch_t) {
+        uint32_t bytes[2] = {0, 0};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bytes[k / 4] |= (k < left ? byte_of[k] : 0) << (8 * (k % 4));
+        *reinterpret_cast<uint2 *>(a.scales_t + tile_r * a.scale_pitch_t + col) = make_uint2(bytes[0], bytes[1]);
+    }
     __syncthreads();
+    // 16 rows of a column a lane, 8 lanes a line
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        const int c = p * kPassRows + r;
-        const int64_t row = tile_c * kTile + c;                 // of the transpose
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = tile[c * kPitch + l * 8 + k];
-        const uint32_t byte = TILES ? byte_of_tile : scale_byte(most_of_block(magnitude(largest(v))));
-        if (row < a.n_cols)
-            *reinterpret_cast<uint2 *>(a.codes_t + row * a.pitch_t + tile_r * kF8Block + l * 8) =
-                make_uint2(codes_of(v[0], v[1], v[2], v[3], byte), codes_of(v[4], v[5], v[6], v[7], byte));
-        if (l == 0 && row < a.scale_pitch_t) a.scales_t[tile_r * a.scale_pitch_t + row] = row < a.n_cols ? (uint8_t)byte : 0;
+    for (int i = 0; i < kTile / 32; ++i) {
+        const int c = i * 32 + threadIdx.x / 8, part = threadIdx.x % 8, of = c / 8;
+        const uint4 both = reinterpret_cast<const uint4 *>(turned)[(of * 8 + (c % 8 ^ of % 2)) * (kTilePieces / 2) + (part ^ of / 2)];
+        const int64_t row = tile_c * kTile + c;     // of the transpose
+        if (row < a.n_cols) *reinterpret_cast<uint4 *>(a.codes_t + row * a.pitch_t + tile_r * kF8Block + part * 16) = of % 2 ? make_uint4(both.z, both.w, both.x, both.y) : both;
     }
 }
 
