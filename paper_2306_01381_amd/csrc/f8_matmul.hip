@@ -316,13 +316,24 @@ F8Shape f8_shape(int64_t m, int64_t n, int64_t k)
         return s;
     }
     auto padded = [&](int64_t rows, int64_t cols) { return (double)((m + rows - 1) / rows * rows) * (double)((n + cols - 1) / cols * cols); };
-    if (s.steps >= 24 && padded(256, 256) < 1.1 * padded(128, 128) && tiles(F8_256_256, 256, 256) >= 512) return s;
-    if (padded(128, 128) < 1.1 * padded(128, 64) && tiles(F8_128_128, 128, 128) >= 512) return s;
+    auto fits = [&](int64_t rows, int64_t cols) { return padded(rows, cols) < 1.1 * padded(rows == 256 ? 128 : rows, cols / 2); };
+    const int64_t large = tiles(F8_256_256, 256, 256), middle = tiles(F8_128_128, 128, 128);
+    if (s.steps >= 14 && fits(256, 256) && (large + 255) / 256 * 256 * 4 * 18 < middle * 25) {
+        tiles(F8_256_256, 256, 256);
+        return s;
+    }
+    if (fits(128, 128) && tiles(F8_128_128, 128, 128) >= 256) return s;
     if (tiles(F8_128_64, 128, 64) >= 256) return s;
     const int64_t small = tiles(F8_64_64, 64, 64);
-    if (small >= 128 || s.steps < 32) return s;
-    const int64_t blocks = small >= 25 ? tiles(F8_128_64, 128, 64) : small;
-    split(480 / blocks < s.steps / 16 ? 480 / blocks : s.steps / 16);
+    if (s.steps < (small >= 128 ? 128 : 32)) return s;
+    const double least = 1.25 * padded(64, 64);
+    const F8Tile tile = padded(128, 128) <= least ? F8_128_128 : padded(128, 64) <= least ? F8_128_64 : F8_64_64;
+    const int64_t blocks = tile == F8_128_128 ? tiles(tile, 128, 128) : tile == F8_128_64 ? tiles(tile, 128, 64) : small;
+    const int64_t wanted = (tile == F8_128_128 ? 256 : 512) / blocks;
+    if (tile == F8_64_64 || s.steps < wanted * 16) {
+        tiles(F8_64_64, 64, 64);
+        split(480 / small < s.steps / 16 ? 480 / small : s.steps / 16);
+    } else split(wanted);
     return s;
 }
 
@@ -334,7 +345,7 @@ void launch_tiles(const F8MulArgs &g, const F8Shape &s, hipStream_t st)
         case F8_FEW_ROWS: f8_few_rows_kernel<T><<<grid_of((g.written + 31) / 32, kFewWaves * kWave, (uint32_t)s.splits), kFewWaves * kWave, 0, st>>>(g); break;
         case F8_64_64:    f8_matmul_kernel<T, EXACT, 64, 64, 4><<<blocks, kBlock, 0, st>>>(g); break;
         case F8_128_64:   f8_matmul_kernel<T, EXACT, 128, 64, 3><<<blocks, kBlock, 0, st>>>(g); break;
-        case F8_128_128:  f8_matmul_kernel<T, EXACT, 128, 128, 4><<<blocks, kBlock, 0, st>>>(g); break;
+        case F8_128_128:  f8_matmul_kernel<T, EXACT, 128, 128, 3><<<blocks, kBlock, 0, st>>>(g); break;
         case F8_256_256:  f8_matmul_kernel<T, EXACT, 256, 256, 4><<<blocks, kBlock, 0, st>>>(g); break;
     }
 }
