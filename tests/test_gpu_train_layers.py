@@ -1,0 +1,156 @@
+"""DenseLayer with products in 8 bits and dropout, Embedding and ClassLoss against their definitions in float64, and the example that puts them together.  u = 2^-24; tolerances as in
+test_gpu_train.py."""
+import importlib.util
+import os
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from oracle import dense as D                                        # noqa: E402
+from oracle import train as O                                        # noqa: E402
+from paper_2306_01381_amd import binding as B                      # noqa: E402
+from paper_2306_01381_amd.dense import ClassLoss, DenseLayer, Embedding  # noqa: E402
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _need_gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    B.lib()
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _held(x, tiles=False):
+    return O.f8_values(*O.f8_quantize(x, tiles), x.shape[1])
+
+
+@pytest.mark.parametrize("rows,n_in,n_out,drop", [(300, 70, 41, 0.0), (2000, 128, 64, 0.5), (517, 602, 256, 0.1)])
+def test_a_step_of_the_layer_in_8_bits_is_its_definition(rows, n_in, n_out, drop):
+    """Each call's result against the definition applied to what the layer held before it, so that no rounding of a code can fall on the other side."""
+    print("layer in 8 bits", rows, n_in, n_out, drop, flush=True)
+    sys.stdout.flush()
+    rng = np.random.default_rng(rows)
+    layer = DenseLayer(rows, n_in, n_out, DEV, seed=3, bits=8, drop=drop)
+    x = torch.from_numpy(rng.standard_normal((rows, n_in))).float().to(DEV)
+    dy = torch.from_numpy(rng.standard_normal((rows, n_out)) * 1e-3).float().to(DEV)
+    weight = _np(layer.weight)
+    for training in (False, True):
+        y = layer.forward(x, training)
+        x8, w8, z = _held(_np(x)), _held(weight, True), _np(layer.z)
+        assert np.all(np.abs(z - x8 @ w8.T) <= 2 * U * (n_in / 64 + 16) * (np.abs(x8) @ np.abs(w8).T) + 1e-38)
+        want, mean, rstd = D.layernorm(z, 1.0, 0.0, np.float32(1e-5))
+        keep, factor = O.dropped(rows, n_out, drop if training else 0.0, layer.seed + layer.drops)
+        want = np.where(keep, want * factor, 0.0)
+        assert np.max(np.abs(_np(y) - want)) <= 1e-5 * np.max(np.abs(want)) and np.array_equal(_np(y) == 0, want == 0)
+    assert layer.drops == (drop > 0)
+    dx = layer.backward(dy)
+    dz = _np(layer.dz)
+    given = np.where(keep, _np(dy) * factor, 0.0)
+    want, dgamma, dbeta = D.layernorm_backward(z, given, *_np(layer.stats).T, 1.0)
+    assert np.max(np.abs(dz - want)) <= 1e-5 * np.max(np.abs(want))
+    assert np.max(np.abs(_np(layer.dgamma) - dgamma)) <= 1e-5 * np.max(np.abs(dgamma)) and np.max(np.abs(_np(layer.dbeta) - dbeta)) <= 1e-5 * np.max(np.abs(dbeta))
+    by_rows, by_columns, xt8 = _held(dz), _held(dz.T), _held(_np(x).T)
+    assert np.all(np.abs(_np(dx) - by_rows @ w8) <= 2 * U * (n_out / 64 + 16) * (np.abs(by_rows) @ np.abs(w8)) + 1e-38)
+    assert np.all(np.abs(_np(layer.dweight) - by_columns @ xt8.T) <= 2 * U * (rows / 64 + 16) * (np.abs(by_columns) @ np.abs(xt8).T) + 1e-38)
+    layer.update(0.02)
+    codes, scales = O.f8_quantize(_np(layer.weight), True)
+    assert np.array_equal(layer.w4[0].cpu().numpy(), codes) and np.array_equal(layer.w4[1].cpu().numpy(), scales)
+    codes, scales = O.f8_quantize(_np(layer.weight).T, True)
+    assert np.array_equal(layer.wt4[0].cpu().numpy(), codes) and np.array_equal(layer.wt4[1].cpu().numpy(), scales)
+
+
+def test_a_layer_in_4_bits_drops_too():
+    layer, plain = (DenseLayer(200, 40, 30, DEV, seed=5, drop=d) for d in (0.4, 0.0))
+    x = torch.randn(200, 40, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV)
+    seen = []
+    for step in range(2):
+        y, full = layer.forward(x), plain.forward(x)
+        keep, factor = O.dropped(200, 30, 0.4, layer.seed + layer.drops)
+        assert torch.equal(y.cpu(), torch.where(torch.from_numpy(keep), full.cpu() * torch.tensor(factor, dtype=torch.float32), 0.0))
+        seen.append(keep)
+    assert not np.array_equal(*seen)                # other elements each time
+    assert torch.equal(layer.forward(x, training=False), full)
+
+
+def test_embedding_and_its_updates():
+    rng = np.random.default_rng(2)
+    table = torch.from_numpy(rng.standard_normal((90, 33))).float()
+    nodes = Embedding(90, 33, 500, DEV, scale=2.0, table=table)
+    ids = torch.from_numpy(rng.integers(-1, 80, 500)).int().to(DEV)
+    dy = torch.from_numpy(rng.standard_normal((500, 33))).float().to(DEV)
+    assert np.array_equal(_np(nodes.forward(ids)), O.embedding(table.double().numpy(), ids.cpu().numpy(), 2.0))
+    want = O.embedding_gradient(_np(dy), ids.cpu().numpy(), 90, 2.0)
+    tol = 64 * U * O.embedding_gradient(np.abs(_np(dy)), ids.cpu().numpy(), 90, 2.0)
+    assert np.all(np.abs(_np(nodes.backward(dy)) - want) <= tol)
+    nodes.descend(dy, 0.1)
+    assert np.all(np.abs(_np(nodes.table) - (table.double().numpy() - 0.1 * want)) <= 0.1 * tol + 4 * U * (np.abs(table.double().numpy()) + np.abs(want)))
+    assert torch.equal(nodes.table[80:].cpu(), table[80:])
+    nodes.forward(ids, training=False)
+    for call in (lambda: nodes.backward(dy), lambda: nodes.descend(dy, 0.1)):
+        with pytest.raises(RuntimeError):
+            call()
+
+
+def test_class_loss():
+    rng = np.random.default_rng(4)
+    logits = torch.from_numpy(3 * rng.standard_normal((300, 47))).float().to(DEV)
+    targets = rng.integers(-1, 47, 300)
+    n = int((targets >= 0).sum())
+    loss, td = ClassLoss(300, 47, DEV), torch.from_numpy(targets).int().to(DEV)
+    logp, most, rest, entropy = O.log_probabilities(_np(logits))
+    got = loss.forward(logits, td)
+    assert np.allclose(_np(got), np.where(targets >= 0, logp[np.arange(300), np.maximum(targets, 0)], 0.0), atol=1e-5) and np.allclose(_np(loss.entropy), entropy, atol=1e-5)
+    want = O.logprob_gradient(_np(logits), targets, most, rest, entropy, np.ones(300), np.zeros(300), -1.0 / n)
+    assert np.allclose(_np(loss.backward(logits, td, n)), want, atol=1e-6 / n, rtol=1e-5)
+    top, classes = loss.likeliest(logits, 3)
+    assert np.array_equal(classes.cpu().numpy(), O.largest(_np(logits), 3)) and np.allclose(_np(top), np.take_along_axis(logp, O.largest(_np(logits), 3), 1), atol=1e-5)
+
+
+def _example():
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_nodes.py")
+    spec = importlib.util.spec_from_file_location("train_nodes", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    return example
+
+
+def test_the_example_runs():
+    losses = _example().train(steps=12, say=lambda *w: print(*w, flush=True))
+    assert len(losses) == 13 and np.isfinite(losses).all()
+
+
+def test_the_examples_gradients_are_its_loss_slopes():
+    """Along the table's gradient: the loss of the model with its first layer's rows as they are, in float64 and without the second layer's rounding, which is what rounding to nearest passes over.  Codes
+    are off by up to 2^-4 of a value, independently; over 600 x 24 values their share of the slope averages out to below a tenth."""
+    rng = np.random.default_rng(6)
+    rows, n_in, hidden, classes = 600, 40, 24, 9
+    model = _example().NodeClassifier(rows, n_in, hidden, classes, DEV)
+    x = torch.from_numpy(rng.standard_normal((rows, n_in))).float().to(DEV)
+    ids = torch.from_numpy(rng.permutation(rows)).int().to(DEV)
+    targets = torch.from_numpy(rng.integers(-1, classes, rows)).int().to(DEV)
+    n = int((targets >= 0).sum())
+    logits = model.forward(x, ids)
+    model.loss.forward(logits, targets)
+    between = model.backward(logits, targets, n)
+    dtable = _np(model.nodes.backward(between))
+    y, w = _np(model.first.y), _np(model.second.weight)
+    picked = targets.cpu().numpy()
+
+    def loss(table):
+        h = y + O.embedding(table, ids.cpu().numpy(), 0.1)
+        z = D.layernorm(h @ w.T, 1.0, 0.0, 1e-5)[0]
+        return -O.log_probabilities(z)[0][np.arange(rows), np.maximum(picked, 0)][picked >= 0].sum() / n
+    table, t = _np(model.nodes.table), 1e-3
+    along = dtable / np.sqrt((dtable ** 2).sum())
+    slope = (loss(table + t * along) - loss(table - t * along)) / (2 * t)
+    assert abs((dtable * along).sum() - slope) <= 0.1 * slope
