@@ -1087,9 +1087,12 @@ def adaqp_orthogonalize(g: torch.Tensor, out: torch.Tensor, coefficients, eps: f
 # What was said above of outputs whose rows are whole 128-byte lines holds for these calls too.
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", lambda: torch.cuda.current_device())      # without the check of whether torch has begun with the GPU: tensors are there
+
+
 def _place(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> Optional[int]:
     """The stream's handle.  Raises where the tensors do not lie on its device (None: the current one)."""
-    device = torch.cuda.current_device() if stream is None else stream.device_index
+    device = _current_device() if stream is None else stream.device_index
     for t in tensors:
         if t is not None and t.get_device() != device:
             raise ValueError(f"a tensor lies on {t.device}, the call's stream on device {device}")

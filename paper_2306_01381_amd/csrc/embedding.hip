@@ -205,7 +205,7 @@ __global__ __launch_bounds__(kCountThreads) void sort_few_kernel(const int32_t *
     for (int i = 0; i < kLoads; ++i) {
         const int32_t j = i * kCountThreads + threadIdx.x;
         if (j < all) {                              // below zero is large
-            auto one = [&](int k) { return j * 4 + k < n ? min(v[i][k], n_entries) : ~0u; };
+            auto one = [&](int k) { return j * 4 + k < n ? min(v[i][k], n_entries) : 0x7FFFFFFFu; };      // behind the last: below none
             keys[j] = make_uint4(one(0), one(1), one(2), one(3));
         }
     }
@@ -213,19 +213,28 @@ __global__ __launch_bounds__(kCountThreads) void sort_few_kernel(const int32_t *
     const uint32_t *flat = reinterpret_cast<const uint32_t *>(keys);
     const uint32_t key = flat[min(mine, n - 1)];
     int32_t before = 0;
-    if (end * 4 <= first || begin * 4 >= first + kCountItems) {
-        const uint32_t bound = end * 4 <= first ? key + 1 : key;   // equal ones are before it if their place is
-#pragma unroll 8
-        for (int32_t j = begin; j < end; ++j) {
+    // Of the fours from `at` on: below 2^31 both, k < bound is the sign of k - bound, and 32 of those make a word.
+    auto count = [&](int32_t at, int32_t end, uint32_t bound) {
+        auto four = [&](uint32_t word, int32_t j) {
             const uint4 k = keys[j];
-            before += k.x < bound ? 1 : 0;
-            before += k.y < bound ? 1 : 0;
-            before += k.z < bound ? 1 : 0;
-            before += k.w < bound ? 1 : 0;
+            word = __builtin_amdgcn_alignbit(word, k.x - bound, 31);
+            word = __builtin_amdgcn_alignbit(word, k.y - bound, 31);
+            word = __builtin_amdgcn_alignbit(word, k.z - bound, 31);
+            return __builtin_amdgcn_alignbit(word, k.w - bound, 31);
+        };
+        for (; at + 8 <= end; at += 8) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) word = four(word, at + i);
+            before += __popc(word);
         }
-    } else
-#pragma unroll 4
-        for (int32_t j = begin * 4; j < end * 4; ++j) before += flat[j] < (j < mine ? key + 1 : key) ? 1 : 0;
+        for (; at < end; ++at) before += __popc(four(0, at));
+    };
+    // in the workgroup's own ids equal ones are before an id if their place is; in those below all are, above none
+    const int32_t own = min(max(first / 4, begin), end), above = min(max((first + kCountItems) / 4, begin), end);
+    count(begin, own, key + 1);
+    for (int32_t j = own * 4; j < above * 4; ++j) before += flat[j] < (j < mine ? key + 1 : key) ? 1 : 0;
+    count(above, end, key);
     part[slice][threadIdx.x % kCountItems] = before;
     __syncthreads();
     if (threadIdx.x >= kCountItems || mine >= n) return;
