@@ -30,7 +30,7 @@ struct LookArgs {
     float scale;
 };
 
-template <typename E, typename T>
+template <typename E, typename T, bool ONCE>
 __global__ __launch_bounds__(kBlock) void lookup_kernel(LookArgs a)
 {
     constexpr int kEach = 2;
@@ -54,7 +54,7 @@ __global__ __launch_bounds__(kBlock) void lookup_kernel(LookArgs a)
     }
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
-        if (first + e * kBlock < a.pieces) store_piece<T, 8>((T *)a.out + row[e] * a.ldo + col[e], a.written - col[e], x[e]);
+        if (first + e * kBlock < a.pieces) store_piece<T, 8, ONCE>((T *)a.out + row[e] * a.ldo + col[e], a.written - col[e], x[e]);
 }
 
 // ---- sort --------------------------------------------------------------------------------------------------------------------------------
@@ -352,7 +352,7 @@ struct GradArgs {
 };
 
 // Of LANES lanes with V columns each, the runs of a chunk.
-template <typename T, int LANES, int V, int CHUNK>
+template <typename T, int LANES, int V, int CHUNK, bool ONCE>
 __device__ __forceinline__ void walk_chunk(const GradArgs &a, int64_t chunk, int32_t col)
 {
     constexpr int kAtOnce = 8, kHeld = LANES < CHUNK ? CHUNK / LANES : 1;
@@ -404,7 +404,7 @@ __device__ __forceinline__ void walk_chunk(const GradArgs &a, int64_t chunk, int
             id[u] = held(held_id, p);
             const int64_t place = held(held_place, p);
             const bool there = at + u < n && place >= 0 && place < a.n_ids && left > 0 && id[u] < a.n_entries;
-            if (there) load_piece<T, V>((const T *)a.dy, place * a.lddy + col, left, a.span, v[u]);
+            if (there) load_piece<T, V, ONCE>((const T *)a.dy, place * a.lddy + col, left, a.span, v[u]);
 #pragma unroll
             for (int k = 0; k < V; ++k) v[u][k] = there ? v[u][k] : 0.0f;
         }
@@ -472,7 +472,7 @@ __device__ __forceinline__ void clear_entries(const GradArgs &a, int64_t tile, u
     }
 }
 
-template <typename T, int LANES, int V, int CHUNK>
+template <typename T, int LANES, int V, int CHUNK, bool ONCE>
 __global__ __launch_bounds__(kBlock) void embedding_runs_kernel(GradArgs a)
 {
     __shared__ uint8_t named[kWavesPerBlock][kWave];
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(kBlock) void embedding_runs_kernel(GradArgs a)
     constexpr int kGroups = kBlock / LANES;
     const int group = LANES == kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / LANES) : threadIdx.x / LANES;
     const int64_t flat = at * kGroups + group, chunk = flat / a.slabs, slab = flat - chunk * a.slabs;
-    if (chunk < a.chunks) walk_chunk<T, LANES, V, CHUNK>(a, chunk, (int32_t)(slab * LANES + threadIdx.x % LANES) * V);       // lanes behind the columns, too: they hold ids
+    if (chunk < a.chunks) walk_chunk<T, LANES, V, CHUNK, ONCE>(a, chunk, (int32_t)(slab * LANES + threadIdx.x % LANES) * V);       // lanes behind the columns, too: they hold ids
 }
 
 // Of each run that begins in a chunk and goes on behind it: the chunk's tail and the heads of the chunks that it covers.  A wave has a chunk; where the heads are many all waves of the workgroup
@@ -595,8 +595,9 @@ void launch_runs(GradArgs &a, hipStream_t st)
     a.run_blocks = (a.chunks * a.slabs + kGroups - 1) / kGroups;
     const int64_t clear = a.accumulate ? 0 : ((a.n_entries + a.clear - 1) / a.clear + kWavesPerBlock - 1) / kWavesPerBlock;
     const dim3 grid = grid_of(a.run_blocks + clear, kBlock);
-    if (a.chunk == kShortChunk) embedding_runs_kernel<T, LANES, V, kShortChunk><<<grid, kBlock, 0, st>>>(a);
-    else                        embedding_runs_kernel<T, LANES, V, kLongChunk><<<grid, kBlock, 0, st>>>(a);
+    if (a.chunk == kShortChunk)               embedding_runs_kernel<T, LANES, V, kShortChunk, false><<<grid, kBlock, 0, st>>>(a);
+    else if (passes_caches(a.span, sizeof(T))) embedding_runs_kernel<T, LANES, V, kLongChunk, true><<<grid, kBlock, 0, st>>>(a);
+    else                                      embedding_runs_kernel<T, LANES, V, kLongChunk, false><<<grid, kBlock, 0, st>>>(a);
 }
 
 template <typename T>
@@ -639,10 +640,14 @@ extern "C" int adaqp_embedding_forward(const void *table_dev, int64_t ldt, int64
     a.pieces_of_row = divider(each, (int64_t)a.pieces);
     const dim3 grid = grid_of((int64_t)((a.pieces + 2 * kBlock - 1) / (2 * kBlock)), kBlock);
     const hipStream_t st = (hipStream_t)stream;
-    if (table_type == ADAQP_F32 && type == ADAQP_F32) lookup_kernel<float, float><<<grid, kBlock, 0, st>>>(a);
-    else if (table_type == ADAQP_F32)                 lookup_kernel<float, __bf16><<<grid, kBlock, 0, st>>>(a);
-    else if (type == ADAQP_F32)                       lookup_kernel<__bf16, float><<<grid, kBlock, 0, st>>>(a);
-    else                                              lookup_kernel<__bf16, __bf16><<<grid, kBlock, 0, st>>>(a);
+    auto go = [&](auto e, auto t) {
+        if (passes_caches(n_ids * ldo, element_bytes(type))) lookup_kernel<decltype(e), decltype(t), true><<<grid, kBlock, 0, st>>>(a);
+        else                                                 lookup_kernel<decltype(e), decltype(t), false><<<grid, kBlock, 0, st>>>(a);
+    };
+    if (table_type == ADAQP_F32 && type == ADAQP_F32) go(0.0f, 0.0f);
+    else if (table_type == ADAQP_F32)                 go(0.0f, (__bf16)0.0f);
+    else if (type == ADAQP_F32)                       go((__bf16)0.0f, 0.0f);
+    else                                              go((__bf16)0.0f, (__bf16)0.0f);
     ADAQP_HIP_TRY(hipGetLastError());
     return ADAQP_OK;
 }

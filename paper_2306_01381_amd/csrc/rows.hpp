@@ -28,22 +28,37 @@ inline Divider divider(int64_t by, int64_t most)
 // Elements from a matrix's first to its last.
 inline int64_t matrix_span(int64_t n_rows, int64_t ld, int64_t cols) { return n_rows > 0 ? (n_rows - 1) * ld + cols : 0; }
 
-// The N elements at `at`, of which the first n are the row's; the others are anything.
-template <typename T, int N>
+// Vectors aligned to an element only, for accesses that say so to the caches.
+template <typename T, int N> using loose_vec = T __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+
+// Whether a matrix of this span, read or written once, drives more out of the 256 MiB of cache before the memory than it brings there.  Smaller ones may themselves be read from it.
+inline bool passes_caches(int64_t span, int64_t bytes) { return span * bytes > ((int64_t)192 << 20); }
+
+// The N elements at `at`, of which the first n are the row's; the others are anything.  ONCE: nothing reads them soon again.
+template <typename T, int N, bool ONCE = false>
 __device__ __forceinline__ void load_piece(const T *base, int64_t at, int n, int64_t span, float (&v)[N])
 {
-    if (at + N <= span) load_loose<T, N>(base + at, v);
-    else
+    if (at + N <= span) {
+        if constexpr (ONCE) {
+            const loose_vec<T, N> w = __builtin_nontemporal_load(reinterpret_cast<const loose_vec<T, N> *>(base + at));
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] = (float)w[k];
+        } else load_loose<T, N>(base + at, v);
+    } else
 #pragma unroll
         for (int k = 0; k < N; ++k) v[k] = k < n ? (float)base[at + k] : 0.0f;
 }
 
 // The first n of N elements, n >= 0.
-template <typename T, int N>
+template <typename T, int N, bool ONCE = false>
 __device__ __forceinline__ void store_piece(T *to, int n, const float (&v)[N])
 {
-    if (n >= N) store_loose<T, N>(to, v);
-    else
+    if (n >= N) {
+        if constexpr (ONCE) {
+            const loose_vec<T, N> w = rounded<T, N>(v);
+            __builtin_nontemporal_store(w, reinterpret_cast<loose_vec<T, N> *>(to));
+        } else store_loose<T, N>(to, v);
+    } else
 #pragma unroll
         for (int k = 0; k < N; ++k)
             if (k < n) to[k] = (T)v[k];
