@@ -11,6 +11,10 @@
 //
 // Where the tiles are few, k is split over workgroups; the parts' sums, fp32, are added in order by a second kernel.  With at most 32 rows nothing is used
 // twice but those: a workgroup takes 32 columns of out, its eight waves share the lines of k and read them into registers.
+//
+// What bounds it: large products the matrix cores and power.  8192 x 8192 x 4096, bf16 out, takes 227 to 250 us (2.2 to 2.4 PFLOP/s; zeros, which draw less, 182); of a tile's 57 us its first loads and its stores take 6, with the
+// matrix cores idle.  With fp32 outputs 425 us, 1.3 PFLOP/s, what a library's bf16 product reaches on this card (1.2).  Shallow products the output: 179 000 x 256, k = 300, bf16 out, 34 us (149 MB, 4.3 TB/s).  Deep ones the operands
+// and the conversions: 256 x 602, k = 58 000, fp32 out, 26 us and 5 to add up the parts.  Few rows their waits: 5 x 8192, k = 4096, 8 us (34 MB, 4.2 TB/s).
 #include "f8.hpp"
 #include "lines.hpp"
 #include "products.hpp"
@@ -291,6 +295,13 @@ struct F8Shape {
     int64_t tiles_m, tiles_n, steps, splits, steps_per_split, bytes;
 };
 
+// us of tiles of 256 x 256 (four steps under way), 128 x 128 (three; with four, and two workgroups a CU instead of three, 40 for 33 in the first line) and 128 x 64 (three), bf16 outputs:
+//     179 000 x 256 x 300    46   33   38       8192 x 8192 x 256    52   38   44       8192 x 8192 x 640    72   66   85
+//     8192 x 8192 x 1024     87   98  130       4096^3               63   88  124       3584 x 3584 x 4096   52   75   97
+//     2048 x 4096 x 4096     48   45   63       1024 x 4096 x 4096   44   25   32       2304^3               30   25   27
+// A large tile takes 0.72 of the time of its four middle ones where the CUs are full, and a round of large tiles that does not fill them takes as long: 256 x 256 where its rounds so counted are fewer.
+// k is split where tiles of 64 x 64 leave half of the CUs idle, or a quarter with 8192 columns and more, so that middle tiles fill the CUs once (256 x 602, k = 58 000, 10 tiles: 16, 24, 32, 48 parts 24, 20, 24, 21 us without the
+// joining), in parts of at least 16 steps; shorter ones in tiles of 64 x 64 (512 x 512, k = 8192, 13 us with the joining, middle tiles 18).
 F8Shape f8_shape(int64_t m, int64_t n, int64_t k)
 {
     F8Shape s{};
