@@ -1090,29 +1090,52 @@ def adaqp_orthogonalize(g: torch.Tensor, out: torch.Tensor, coefficients, eps: f
 _current_device = getattr(torch._C, "_cuda_getDevice", lambda: torch.cuda.current_device())      # without the check of whether torch has begun with the GPU: tensors are there
 
 
-def _place(stream: Optional[torch.cuda.Stream], *tensors: Optional[torch.Tensor]) -> Optional[int]:
+def _place(stream: Optional[torch.cuda.Stream], first: torch.Tensor, *others: Optional[torch.Tensor]) -> Optional[int]:
     """The stream's handle.  Raises where the tensors do not lie on its device (None: the current one)."""
-    device = _current_device() if stream is None else stream.device_index
-    for t in tensors:
+    device = first.get_device()
+    for t in others:
         if t is not None and t.get_device() != device:
-            raise ValueError(f"a tensor lies on {t.device}, the call's stream on device {device}")
+            if t.get_device() < 0:
+                raise TypeError(f"a tensor of the call lies on {t.device}, not on a device")
+            raise ValueError(f"the call's tensors lie on {first.device} and on {t.device}")
+    if device < 0:
+        raise TypeError(f"a tensor of the call lies on {first.device}, not on a device")
+    if device != (_current_device() if stream is None else stream.device_index):
+        raise ValueError(f"the call's tensors lie on {first.device}, its stream does not")
     return (_current_raw_stream(device) if stream is None else stream.cuda_stream) or None
 
 
-def _ints(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
-    p = _dev(t, torch.int32, name)
-    if t is not None and t.numel() < n:
+# The two below leave it to _place to find what lies on no device.
+
+def _cells(t: torch.Tensor, dim: int, name: str) -> Tuple[int, int, int, int]:
+    """_elements, of a tensor that _place is asked about."""
+    shape, stride, kind = t.shape, t.stride(), _TYPES.get(t.dtype)
+    if kind is None or len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise TypeError(f"{name} must be a 2-D fp32 or bf16 device tensor with unit column stride")
+    rows, cols = shape
+    if cols < dim:
+        raise ValueError(f"{name} has {cols} columns, {dim} are wanted")
+    return t.data_ptr(), rows, stride[0] if rows > 1 else max(stride[0], cols), kind
+
+
+def _flat(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, name: str) -> Optional[int]:
+    """The pointer of a contiguous tensor of at least n elements."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be contiguous and {dtype}")
+    if t.numel() < n:
         raise ValueError(f"{name} has {t.numel()} elements, {n} are wanted")
-    return p
+    return t.data_ptr()
 
 
 def adaqp_embedding_forward(table: torch.Tensor, dim: int, ids: torch.Tensor, scale: float, out: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """out: rows that are whole 128-byte lines are written to their last line's end, zeros behind column `dim`."""
-    tp, entries, ldt, kind_t = _elements(table, dim, "table")
-    op, rows, ldo, kind = _elements(out, dim, "out")
+    tp, entries, ldt, kind_t = _cells(table, dim, "table")
+    op, rows, ldo, kind = _cells(out, dim, "out")
     if ids.numel() != rows:
         raise ValueError(f"{ids.numel()} ids, out has {rows} rows")
-    ip = _ints(ids, rows, "ids")
+    ip = _flat(ids, torch.int32, rows, "ids")
     st = _place(stream, table, ids, out)
     _check(lib().adaqp_embedding_forward(tp, ldt, entries, dim, kind_t, ip, rows, scale, op, ldo, kind, st), "adaqp_embedding_forward")
 
@@ -1124,8 +1147,8 @@ def adaqp_embedding_sort_workspace_bytes(n_ids: int, n_entries: int) -> int:
 def adaqp_embedding_sort(ids: torch.Tensor, n_entries: int, sorted_ids: torch.Tensor, order: torch.Tensor, workspace: Optional[torch.Tensor],
                          stream: Optional[torch.cuda.Stream] = None) -> None:
     n = ids.numel()
-    ip, sp, op = _ints(ids, n, "ids"), _ints(sorted_ids, n, "sorted_ids"), _ints(order, n, "order")
-    wp, wn = _workspace(workspace)
+    ip, sp, op = _flat(ids, torch.int32, n, "ids"), _flat(sorted_ids, torch.int32, n, "sorted_ids"), _flat(order, torch.int32, n, "order")
+    wp, wn = _flat(workspace, torch.uint8, 0, "workspace"), 0 if workspace is None else workspace.numel()
     st = _place(stream, ids, sorted_ids, order, workspace)
     _check(lib().adaqp_embedding_sort(ip, n, n_entries, sp, op, wp, wn, st), "adaqp_embedding_sort")
 
@@ -1137,12 +1160,12 @@ def adaqp_embedding_backward_workspace_bytes(n_ids: int, dim: int) -> int:
 def adaqp_embedding_backward(dy: torch.Tensor, dim: int, sorted_ids: torch.Tensor, order: torch.Tensor, scale: float, accumulate: bool, dtable: torch.Tensor,
                              workspace: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
     """dtable: rows that are whole 128-byte lines are written to their last line's end, zeros behind column `dim`; with `accumulate` only columns are."""
-    yp, rows, lddy, kind = _elements(dy, dim, "dy")
-    tp, entries, ldd, kind_t = _elements(dtable, dim, "dtable")
+    yp, rows, lddy, kind = _cells(dy, dim, "dy")
+    tp, entries, ldd, kind_t = _cells(dtable, dim, "dtable")
     if kind_t != 0:
         raise TypeError("dtable must be fp32")
-    sp, op = _ints(sorted_ids, rows, "sorted_ids"), _ints(order, rows, "order")
-    wp, wn = _workspace(workspace)
+    sp, op = _flat(sorted_ids, torch.int32, rows, "sorted_ids"), _flat(order, torch.int32, rows, "order")
+    wp, wn = _flat(workspace, torch.uint8, 0, "workspace"), 0 if workspace is None else workspace.numel()
     st = _place(stream, dy, sorted_ids, order, dtable, workspace)
     _check(lib().adaqp_embedding_backward(yp, lddy, rows, dim, kind, sp, op, entries, scale, int(bool(accumulate)), tp, ldd, wp, wn, st), "adaqp_embedding_backward")
 
@@ -1151,13 +1174,11 @@ def adaqp_dropout(x: torch.Tensor, dim: int, p: float, seed: int, y: torch.Tenso
                   counter: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """counter: one int64 in device memory, added to the seed when the call runs.  y: rows that are whole 128-byte lines are written to their last line's end, zeros behind
     column `dim`."""
-    xp, rows, ldx, kind = _elements(x, dim, "x")
-    yp, rows_y, ldy, kind_y = _elements(y, dim, "y")
-    ap, rows_a, lda, kind_a = (None, rows, 0, kind) if add is None else _elements(add, dim, "add")
+    xp, rows, ldx, kind = _cells(x, dim, "x")
+    yp, rows_y, ldy, kind_y = _cells(y, dim, "y")
+    ap, rows_a, lda, kind_a = (None, rows, 0, kind) if add is None else _cells(add, dim, "add")
     _same("adaqp_dropout", (rows, kind), (rows_y, kind_y), (rows_a, kind_a))
-    cp = _dev(counter, torch.int64, "counter")
-    if counter is not None and counter.numel() < 1:
-        raise ValueError("counter has no element")
+    cp = _flat(counter, torch.int64, 1, "counter")
     st = _place(stream, x, y, add, counter)
     _check(lib().adaqp_dropout(xp, ldx, ap, lda, rows, dim, kind, p, seed & (2**64 - 1), first_row, cp, yp, ldy, st), "adaqp_dropout")
 
@@ -1182,7 +1203,7 @@ def _f8(packed: Optional[Tuple[torch.Tensor, torch.Tensor]], n_rows: Optional[in
         return None, None, n_rows
     codes, scales = packed
     rows = codes.shape[0] if n_rows is None else n_rows
-    cp, sp = _dev(codes, torch.uint8, f"{name} codes"), _dev(scales, torch.uint8, f"{name} scales")
+    cp, sp = _flat(codes, torch.uint8, 0, name), _flat(scales, torch.uint8, 0, name)
     chunks = -(-n_cols // 128)
     if codes.shape != (rows, 128 * chunks) or scales.shape != (chunks, -(-rows // 16) * 16):
         raise ValueError(f"{name}: codes {tuple(codes.shape)} and scales {tuple(scales.shape)} are not those of {rows} rows and {n_cols} columns")
@@ -1192,7 +1213,7 @@ def _f8(packed: Optional[Tuple[torch.Tensor, torch.Tensor]], n_rows: Optional[in
 def adaqp_f8_quantize(x: torch.Tensor, n_cols: int, blocks: int, packed: Optional[Tuple[torch.Tensor, torch.Tensor]],
                       packed_t: Optional[Tuple[torch.Tensor, torch.Tensor]], stream: Optional[torch.cuda.Stream] = None) -> None:
     """packed, packed_t: (codes, scales) of the matrix and of its transpose, as f8_empty makes them."""
-    xp, rows, ld, kind = _elements(x, n_cols, "x")
+    xp, rows, ld, kind = _cells(x, n_cols, "x")
     cp, sp, _ = _f8(packed, rows, n_cols, "packed")
     ctp, stp, _ = _f8(packed_t, n_cols, rows, "packed_t")
     st = _place(stream, x, *(packed or ()), *(packed_t or ()))
@@ -1201,7 +1222,7 @@ def adaqp_f8_quantize(x: torch.Tensor, n_cols: int, blocks: int, packed: Optiona
 
 def adaqp_f8_dequantize(packed: Tuple[torch.Tensor, torch.Tensor], n_cols: int, x: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
     """x: rows that are whole 128-byte lines are written to their last line's end, zeros behind column n_cols."""
-    xp, rows, ld, kind = _elements(x, n_cols, "x")
+    xp, rows, ld, kind = _cells(x, n_cols, "x")
     cp, sp, _ = _f8(packed, rows, n_cols, "packed")
     st = _place(stream, x, *packed)
     _check(lib().adaqp_f8_dequantize(cp, sp, rows, n_cols, xp, ld, kind, st), "adaqp_f8_dequantize")
@@ -1216,10 +1237,10 @@ def adaqp_f8_matmul(a: Tuple[torch.Tensor, torch.Tensor], b: Tuple[torch.Tensor,
     """out = a b^T for 8-bit matrices of k columns.  out: rows that are whole 128-byte lines are written to their last line's end, zeros behind b's last row's column."""
     ac, asc, m = _f8(a, None, k, "a")
     bc, bsc, n = _f8(b, None, k, "b")
-    op, rows, ldo, kind = _elements(out, n, "out")
+    op, rows, ldo, kind = _cells(out, n, "out")
     if rows != m:
         raise ValueError(f"out has {rows} rows, a {m}")
-    wp, wn = _workspace(workspace)
+    wp, wn = _flat(workspace, torch.uint8, 0, "workspace"), 0 if workspace is None else workspace.numel()
     st = _place(stream, *a, *b, out, workspace)
     _check(lib().adaqp_f8_matmul(ac, asc, m, bc, bsc, n, k, op, ldo, kind, wp, wn, st), "adaqp_f8_matmul")
 
@@ -1232,17 +1253,17 @@ def adaqp_logprob_forward(logits: torch.Tensor, n_classes: int, targets: Optiona
                           stats: Optional[torch.Tensor] = None, top_logp: Optional[torch.Tensor] = None, top_class: Optional[torch.Tensor] = None,
                           workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """top_logp, top_class: [rows, n_top], both or neither."""
-    xp, rows, ld, kind = _elements(logits, n_classes, "logits")
+    xp, rows, ld, kind = _cells(logits, n_classes, "logits")
     n_top = 0
     for t, name in ((top_logp, "top_logp"), (top_class, "top_class")):
         if t is not None:
             if t.dim() != 2 or t.shape[0] != rows:
                 raise ValueError(f"{name} must have a row for each of {rows}")
             n_top = max(n_top, t.shape[1])
-    tp = _ints(targets, rows, "targets")
-    lp, ep, sp = _vector(logp, rows, "logp"), _vector(entropy, rows, "entropy"), _vector(stats, 2 * rows, "stats")
-    vp, cp = _vector(top_logp, rows * n_top, "top_logp"), _ints(top_class, rows * n_top, "top_class")
-    wp, wn = _workspace(workspace)
+    tp = _flat(targets, torch.int32, rows, "targets")
+    lp, ep, sp = _flat(logp, torch.float32, rows, "logp"), _flat(entropy, torch.float32, rows, "entropy"), _flat(stats, torch.float32, 2 * rows, "stats")
+    vp, cp = _flat(top_logp, torch.float32, rows * n_top, "top_logp"), _flat(top_class, torch.int32, rows * n_top, "top_class")
+    wp, wn = _flat(workspace, torch.uint8, 0, "workspace"), 0 if workspace is None else workspace.numel()
     st = _place(stream, logits, targets, logp, entropy, stats, top_logp, top_class, workspace)
     _check(lib().adaqp_logprob_forward(xp, ld, rows, n_classes, kind, tp, lp, ep, sp, n_top, vp if n_top else None, cp if n_top else None, wp, wn, st), "adaqp_logprob_forward")
 
@@ -1251,11 +1272,11 @@ def adaqp_logprob_backward(logits: torch.Tensor, n_classes: int, targets: Option
                            dlogp: Optional[torch.Tensor], dentropy: Optional[torch.Tensor], scale: float, dlogits: torch.Tensor,
                            stream: Optional[torch.cuda.Stream] = None) -> None:
     """dlogits: rows that are whole 128-byte lines are written to their last line's end, zeros behind column n_classes."""
-    xp, rows, ld, kind = _elements(logits, n_classes, "logits")
-    dp, rows_d, ldd, kind_d = _elements(dlogits, n_classes, "dlogits")
+    xp, rows, ld, kind = _cells(logits, n_classes, "logits")
+    dp, rows_d, ldd, kind_d = _cells(dlogits, n_classes, "dlogits")
     _same("adaqp_logprob_backward", (rows, kind), (rows_d, kind_d))
-    tp = _ints(targets, rows, "targets")
-    sp, ep = _vector(stats, 2 * rows, "stats"), _vector(entropy, rows, "entropy")
-    gp, hp = _vector(dlogp, rows, "dlogp"), _vector(dentropy, rows, "dentropy")
+    tp = _flat(targets, torch.int32, rows, "targets")
+    sp, ep = _flat(stats, torch.float32, 2 * rows, "stats"), _flat(entropy, torch.float32, rows, "entropy")
+    gp, hp = _flat(dlogp, torch.float32, rows, "dlogp"), _flat(dentropy, torch.float32, rows, "dentropy")
     st = _place(stream, logits, targets, stats, entropy, dlogp, dentropy, dlogits)
     _check(lib().adaqp_logprob_backward(xp, ld, rows, n_classes, kind, tp, sp, ep, gp, hp, scale, dp, ldd, st), "adaqp_logprob_backward")

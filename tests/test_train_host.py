@@ -134,8 +134,16 @@ def test_wrappers_refuse_tensors_that_are_not_what_they_name():
                  lambda: B.adaqp_logprob_forward(x, 8, ids, None), lambda: B.adaqp_logprob_backward(x, 8, ids, x, None, None, None, 1.0, x)):
         with pytest.raises(TypeError):
             call()                                  # not on a device
-    with pytest.raises(TypeError):
-        B._ints(torch.zeros(4, dtype=torch.int64), 4, "ids")
+    for t, dtype in ((torch.zeros(4, dtype=torch.int64), torch.int32), (torch.zeros(4, 2)[:, 0], torch.float32)):
+        with pytest.raises(TypeError):
+            B._flat(t, dtype, 4, "t")
+    with pytest.raises(ValueError):
+        B._flat(x, torch.float32, 33, "t")
+    for wrong in (torch.zeros(4, 8, dtype=torch.float64), torch.zeros(8), torch.zeros(8, 4).t()):
+        with pytest.raises(TypeError):
+            B._cells(wrong, 1, "t")
+    with pytest.raises(ValueError):
+        B._cells(x, 9, "t")
 
 
 def test_wrappers_refuse_tensors_of_another_device():
@@ -151,6 +159,9 @@ def test_wrappers_refuse_tensors_of_another_device():
     assert B._place(Stream, On(1), None, On(1)) == 77
     for tensors in ((On(0),), (On(1), On(0)), (On(1), None, On(2))):
         with pytest.raises(ValueError):
+            B._place(Stream, *tensors)
+    for tensors in ((On(-1),), (On(1), On(-1)), (On(-1), On(1)), (On(-1), On(-1))):
+        with pytest.raises((TypeError, ValueError)):
             B._place(Stream, *tensors)
 
 
