@@ -10,7 +10,7 @@
 //
 // Gradient: the sorted places are cut into chunks.  A group of lanes walks a chunk, adds the rows of equal ids in registers and stores the sum of every run that lies in
 // its chunk; of the runs that go on it leaves the parts (the first run's as the chunk's head, the last one's as its tail), and a second kernel adds a tail and the heads
-// behind it.  Entries without a row are found by a search of the sorted ids, 64 places a step, and set to zero beside it in the same launch.  Bound by memory: 131 072 ids, 50 000 x 1024 fp32, 142 us (742 MB, 5.2 TB/s; 178 where the
+// behind it; with many chunks one between them adds heads by blocks of 64.  Entries without a row are found by a search of the sorted ids, 64 places a step, and set to zero beside it in the same launch.  Bound by memory: 131 072 ids, 50 000 x 1024 fp32, 142 us (742 MB, 5.2 TB/s; 178 where the
 // gradient's rows, which are read once, go through the caches) and 14 for the second kernel, whose longest run has 380 heads; 9001 ids, 20 000 x 301 bf16, 10.7 and 5 us, a chain of waits.
 #include "adaqp_train.h"
 #include "rows.hpp"
@@ -345,6 +345,7 @@ struct GradArgs {
     const void *dy;
     const int32_t *sorted, *order;
     float *dtable, *parts;                          // [chunks][head, tail][pitch]
+    float *block_parts;                             // [chunks / kBlockChunks][pitch]; NULL: there are too few
     int64_t lddy, ldd, span, n_ids, n_entries, chunks, pitch;
     int64_t run_blocks;                             // workgroups that walk chunks; those behind them set entries to zero
     int32_t dim, written;                           // columns of dy; of dtable's rows that are written
@@ -492,10 +493,55 @@ __global__ __launch_bounds__(kBlock) void embedding_runs_kernel(GradArgs a)
     if (chunk < a.chunks) walk_chunk<T, LANES, V, CHUNK, ONCE>(a, chunk, (int32_t)(slab * LANES + threadIdx.x % LANES) * V);       // lanes behind the columns, too: they hold ids
 }
 
-// Of each run that begins in a chunk and goes on behind it: the chunk's tail and the heads of the chunks that it covers.  A wave has a chunk; where the heads are many all waves of the workgroup
-// share them.
+// Of chunks [kBlockChunks b, kBlockChunks (b + 1)) that all begin inside the same run, the sum of their heads: few ids with very many places each would leave the next kernel thousands of heads to add in turn.
+constexpr int kBlockChunks = 64;
+
 constexpr int kJoinWaves = 8, kJoinCols = kWave * 4, kFewHeads = 16;
 
+// Adds rows begin, begin + step, ... up to last of `from`, of a pitch in floats, in turn.
+__device__ __forceinline__ void add_rows(const float *from, int64_t pitch, int64_t begin, int64_t last, int step, float (&sum)[4])
+{
+    constexpr int kAtOnce = 8;
+    for (int64_t c = begin; c <= last; c += step * kAtOnce) {
+        float v[kAtOnce][4];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            load_elements<float, 4>(from + min(c + u * step, last) * pitch, v[u]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[u][k] = c + u * step <= last ? v[u][k] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += v[u][k];
+    }
+}
+
+__global__ __launch_bounds__(kJoinWaves * kWave) void embedding_blocks_kernel(GradArgs a)
+{
+    __shared__ float part[kJoinWaves][kJoinCols];
+    const int64_t at = workgroup(), slab = at % a.slabs, block = at / a.slabs, chunk = block * kBlockChunks;
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    if (chunk + kBlockChunks > a.chunks || chunk == 0) return;
+    const int32_t id = a.sorted[chunk * a.chunk];
+    if (a.sorted[chunk * a.chunk - 1] != id || a.sorted[(chunk + kBlockChunks - 1) * a.chunk] != id) return;
+    const int32_t col = (int32_t)slab * kJoinCols + lane * 4;
+    float sum[4] = {};
+    if (col < a.dim) add_rows(a.parts + col, 2 * a.pitch, chunk + wave, chunk + kBlockChunks - 1, kJoinWaves, sum);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[wave][k * kWave + lane] = sum[k];
+    __syncthreads();
+    if (wave != 0 || col >= a.dim) return;
+    float v[4] = {};
+#pragma unroll
+    for (int i = 0; i < kJoinWaves; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] += part[i][k * kWave + lane];
+    store_elements<float, 4, false>(a.block_parts + block * a.pitch + col, v);
+}
+
+// Of each run that begins in a chunk and goes on behind it: the chunk's tail and the heads of the chunks that it covers, those of whole blocks together.  A wave has a chunk; where the heads are many all waves of
+// the workgroup share them.
 __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_join_kernel(GradArgs a)
 {
     __shared__ float part[kJoinWaves][kJoinCols];
@@ -505,22 +551,16 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_join_kernel(Grad
     const int32_t col = (int32_t)slab * kJoinCols + lane * 4;
     const int left = a.dim - col;
     const float *heads = a.parts + col;
-    // heads begin, begin + step, ... up to last
-    auto sum_heads = [&](int64_t begin, int64_t last, int step, float (&sum)[4]) {
-        constexpr int kAtOnce = 8;
-        for (int64_t c = begin; c <= last; c += step * kAtOnce) {
-            float v[kAtOnce][4];
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u) {
-                load_elements<float, 4>(heads + min(c + u * step, last) * 2 * a.pitch, v[u]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) v[u][k] = c + u * step <= last ? v[u][k] : 0.0f;
-            }
-#pragma unroll
-            for (int u = 0; u < kAtOnce; ++u)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) sum[k] += v[u][k];
+    // of the heads begin .. last every step-th from the first-th on
+    auto sum_heads = [&](int64_t begin, int64_t last, int first, int step, float (&sum)[4]) {
+        const int64_t block = (begin + kBlockChunks - 1) / kBlockChunks, blocks = (last + 1) / kBlockChunks;
+        if (!a.block_parts || block >= blocks) {
+            add_rows(heads, 2 * a.pitch, begin + first, last, step, sum);
+            return;
         }
+        add_rows(heads, 2 * a.pitch, begin + first, block * kBlockChunks - 1, step, sum);
+        add_rows(a.block_parts + col, a.pitch, block + first, blocks - 1, step, sum);
+        add_rows(heads, 2 * a.pitch, blocks * kBlockChunks + first, last, step, sum);
     };
     auto store = [&](int32_t id, float (&v)[4]) {
         if (col >= a.written) return;
@@ -551,7 +591,7 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_join_kernel(Grad
                     float v[4] = {};
                     if (left > 0) {
                         load_elements<float, 4>(heads + (chunk * 2 + 1) * a.pitch, v);
-                        sum_heads(chunk + 1, last, 1, v);
+                        sum_heads(chunk + 1, last, 0, 1, v);
                     }
                     store(id, v);
                     last = 0;
@@ -565,7 +605,7 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_join_kernel(Grad
         const int64_t chunk = chunk0 + w, last = last_of[w];
         if (last == 0) continue;
         float sum[4] = {};
-        if (left > 0) sum_heads(chunk + 1 + wave, last, kJoinWaves, sum);
+        if (left > 0) sum_heads(chunk + 1, last, wave, kJoinWaves, sum);
 #pragma unroll
         for (int k = 0; k < 4; ++k) part[wave][k * kWave + lane] = sum[k];
         __syncthreads();
@@ -589,6 +629,8 @@ constexpr int32_t kFewClear = 16;
 int32_t grad_chunk(int64_t n_ids, int32_t dim) { return (n_ids + kLongChunk - 1) / kLongChunk * (((int64_t)dim + 255) / 256) < 4096 ? kShortChunk : kLongChunk; }
 int64_t grad_chunks(int64_t n_ids, int32_t dim) { return (n_ids + grad_chunk(n_ids, dim) - 1) / grad_chunk(n_ids, dim); }
 int64_t grad_pitch(int32_t dim) { return ((int64_t)dim + 7) / 8 * 8; }
+// Blocks of chunks: none below 2048 chunks, where the launch (3 us) costs more than it mostly saves.  65 536 ids of 10 entries x 256 54 us without, 37 with; 9001 of 20 000 x 301, 1126 chunks, 16 and 18.
+int64_t grad_blocks(int64_t n_ids, int32_t dim) { return grad_chunks(n_ids, dim) < 2048 ? 0 : grad_chunks(n_ids, dim) / kBlockChunks; }
 
 template <typename T, int LANES>
 void launch_runs(GradArgs &a, hipStream_t st)
@@ -614,6 +656,11 @@ hipError_t launch_gradient(GradArgs a, hipStream_t st)
     hipError_t err = hipGetLastError();
     if (err != hipSuccess || a.chunks < 2) return err;
     a.slabs = (a.written + kJoinCols - 1) / kJoinCols;
+    if (a.block_parts) {
+        embedding_blocks_kernel<<<grid_of(a.chunks / kBlockChunks * a.slabs, kJoinWaves * kWave), kJoinWaves * kWave, 0, st>>>(a);
+        err = hipGetLastError();
+        if (err != hipSuccess) return err;
+    }
     embedding_join_kernel<<<grid_of((a.chunks - 1 + kJoinWaves - 1) / kJoinWaves * a.slabs, kJoinWaves * kWave), kJoinWaves * kWave, 0, st>>>(a);
     return hipGetLastError();
 }
@@ -710,7 +757,7 @@ extern "C" int adaqp_embedding_backward_workspace_bytes(int64_t n_ids, int32_t d
 {
     if (!bytes_out || n_ids < 0 || dim <= 0) return ADAQP_EINVAL;
     if (n_ids >= kMostIds || dim > kMostDim) return ADAQP_ESIZE;
-    *bytes_out = n_ids > grad_chunk(n_ids, dim) ? (grad_chunks(n_ids, dim) * 2 * grad_pitch(dim) * 4 + 255) / 256 * 256 : 0;
+    *bytes_out = n_ids > grad_chunk(n_ids, dim) ? ((grad_chunks(n_ids, dim) * 2 + grad_blocks(n_ids, dim)) * grad_pitch(dim) * 4 + 255) / 256 * 256 : 0;
     return ADAQP_OK;
 }
 
@@ -740,6 +787,8 @@ extern "C" int adaqp_embedding_backward(const void *dy_dev, int64_t lddy, int64_
     a.chunk = grad_chunk(n_ids, dim);
     a.chunks = grad_chunks(n_ids, dim);
     a.pitch = grad_pitch(dim);
+    const int64_t blocks = grad_blocks(n_ids, dim);
+    a.block_parts = blocks > 0 ? a.parts + a.chunks * 2 * a.pitch : nullptr;
     a.clear = dim >= 128 ? kFewClear : kWave;
     a.written = accumulate ? dim : (int32_t)columns_to_write(dtable_dev, ldd, dim, 4);
     if ((a.chunks + 1) * (((int64_t)a.written + kWave - 1) / kWave + 1) + a.n_entries / kFewClear >= kMostWorkgroups) return ADAQP_ESIZE;
