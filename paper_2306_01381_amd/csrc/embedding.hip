@@ -10,7 +10,7 @@
 //
 // Gradient: the sorted places are cut into chunks.  A group of lanes walks a chunk, adds the rows of equal ids in registers and stores the sum of every run that lies in
 // its chunk; of the runs that go on it leaves the parts (the first run's as the chunk's head, the last one's as its tail), and a second kernel adds a tail and the heads
-// behind it; with many chunks one between them adds heads by blocks of 64.  Entries without a row are found by a search of the sorted ids, 64 places a step, and set to zero beside it in the same launch.  Bound by memory: 131 072 ids, 50 000 x 1024 fp32, 142 us (742 MB, 5.2 TB/s; 178 where the
+// behind it; where entries have very many ids each one between them adds heads by blocks of 64.  Entries without a row are found by a search of the sorted ids, 64 places a step, and set to zero beside it in the same launch.  Bound by memory: 131 072 ids, 50 000 x 1024 fp32, 142 us (742 MB, 5.2 TB/s; 178 where the
 // gradient's rows, which are read once, go through the caches) and 14 for the second kernel, whose longest run has 380 heads; 9001 ids, 20 000 x 301 bf16, 10.7 and 5 us, a chain of waits.
 #include "adaqp_train.h"
 #include "rows.hpp"
@@ -542,6 +542,7 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_blocks_kernel(Gr
 
 // Of each run that begins in a chunk and goes on behind it: the chunk's tail and the heads of the chunks that it covers, those of whole blocks together.  A wave has a chunk; where the heads are many all waves of
 // the workgroup share them.
+template <bool BLOCKS>
 __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_join_kernel(GradArgs a)
 {
     __shared__ float part[kJoinWaves][kJoinCols];
@@ -554,7 +555,7 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_join_kernel(Grad
     // of the heads begin .. last every step-th from the first-th on
     auto sum_heads = [&](int64_t begin, int64_t last, int first, int step, float (&sum)[4]) {
         const int64_t block = (begin + kBlockChunks - 1) / kBlockChunks, blocks = (last + 1) / kBlockChunks;
-        if (!a.block_parts || block >= blocks) {
+        if (!BLOCKS || block >= blocks) {
             add_rows(heads, 2 * a.pitch, begin + first, last, step, sum);
             return;
         }
@@ -629,8 +630,12 @@ constexpr int32_t kFewClear = 16;
 int32_t grad_chunk(int64_t n_ids, int32_t dim) { return (n_ids + kLongChunk - 1) / kLongChunk * (((int64_t)dim + 255) / 256) < 4096 ? kShortChunk : kLongChunk; }
 int64_t grad_chunks(int64_t n_ids, int32_t dim) { return (n_ids + grad_chunk(n_ids, dim) - 1) / grad_chunk(n_ids, dim); }
 int64_t grad_pitch(int32_t dim) { return ((int64_t)dim + 7) / 8 * 8; }
-// Blocks of chunks: none below 2048 chunks, where the launch (3 us) costs more than it mostly saves.  65 536 ids of 10 entries x 256 54 us without, 37 with; 9001 of 20 000 x 301, 1126 chunks, 16 and 18.
+// Blocks of chunks: the workspace has room for them from 2048 chunks on.
 int64_t grad_blocks(int64_t n_ids, int32_t dim) { return grad_chunks(n_ids, dim) < 2048 ? 0 : grad_chunks(n_ids, dim) / kBlockChunks; }
+
+// Ids for each entry from which on the blocks have a launch of their own: the places of a block.  Without and with, fp32: 65 536 ids of 10 entries x 256 53 and 37 us, 131 072 of 40 x 1024
+// 113 and 111; of 256 x 1024 110 and 113, of 50 000 x 1024 147 and 153.  A large table with one very frequent id has none: the host does not know the ids.
+constexpr int64_t kManyPlaces = kBlockChunks * kLongChunk;
 
 template <typename T, int LANES>
 void launch_runs(GradArgs &a, hipStream_t st)
@@ -661,7 +666,9 @@ hipError_t launch_gradient(GradArgs a, hipStream_t st)
         err = hipGetLastError();
         if (err != hipSuccess) return err;
     }
-    embedding_join_kernel<<<grid_of((a.chunks - 1 + kJoinWaves - 1) / kJoinWaves * a.slabs, kJoinWaves * kWave), kJoinWaves * kWave, 0, st>>>(a);
+    const dim3 grid = grid_of((a.chunks - 1 + kJoinWaves - 1) / kJoinWaves * a.slabs, kJoinWaves * kWave);
+    if (a.block_parts) embedding_join_kernel<true><<<grid, kJoinWaves * kWave, 0, st>>>(a);
+    else               embedding_join_kernel<false><<<grid, kJoinWaves * kWave, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -788,7 +795,7 @@ extern "C" int adaqp_embedding_backward(const void *dy_dev, int64_t lddy, int64_
     a.chunks = grad_chunks(n_ids, dim);
     a.pitch = grad_pitch(dim);
     const int64_t blocks = grad_blocks(n_ids, dim);
-    a.block_parts = blocks > 0 ? a.parts + a.chunks * 2 * a.pitch : nullptr;
+    a.block_parts = blocks > 0 && n_ids / n_entries >= kManyPlaces ? a.parts + a.chunks * 2 * a.pitch : nullptr;
     a.clear = dim >= 128 ? kFewClear : kWave;
     a.written = accumulate ? dim : (int32_t)columns_to_write(dtable_dev, ldd, dim, 4);
     if ((a.chunks + 1) * (((int64_t)a.written + kWave - 1) / kWave + 1) + a.n_entries / kFewClear >= kMostWorkgroups) return ADAQP_ESIZE;
