@@ -67,6 +67,7 @@ class DenseLayer:
         self.workspace = torch.empty(need, dtype=torch.uint8, device=dev)       # of one call at a time: they follow one another on a stream
         self.steps = 0
         self.drops = 0                              # forwards that dropped; the seed of their choices is self.seed + self.drops, by another generator tag than the rounding's
+        self.dropped = 0.0                          # the share that the last forward for training dropped
         self.trained_on = False                     # whether xt4 is of the last forward's x
         self._quantize_weight()
 
@@ -88,9 +89,11 @@ class DenseLayer:
             B.adaqp_f8_quantize(x, self.n_in, B.F8_ROWS, self.x4, self.xt4 if training else None)
         self._product(self.x4, self.w4, self.n_in, self.z)
         B.adaqp_layernorm_forward(self.z, self.n_out, self.gamma, self.beta, self.eps, self.y, self.stats)
-        if training and self.drop > 0.0:
+        if training:
+            self.dropped = self.drop
+        if training and self.dropped > 0.0:
             self.drops += 1
-            B.adaqp_dropout(self.y, self.n_out, self.drop, self.seed + self.drops, self.y)
+            B.adaqp_dropout(self.y, self.n_out, self.dropped, self.seed + self.drops, self.y)
         self.trained_on = training
         return self.y
 
@@ -98,8 +101,8 @@ class DenseLayer:
         """dx of the last forward(), and the parameters' gradients in dweight, dgamma and dbeta.  Raises if that was none for training."""
         if not self.trained_on:
             raise RuntimeError("backward() needs a forward(training=True) before it: there is no columns' form of x")
-        if self.drop > 0.0:
-            B.adaqp_dropout(dy, self.n_out, self.drop, self.seed + self.drops, self.dz)
+        if self.dropped > 0.0:
+            B.adaqp_dropout(dy, self.n_out, self.dropped, self.seed + self.drops, self.dz)
             dy = self.dz
         B.adaqp_layernorm_backward(self.z, dy, self.n_out, self.stats, self.gamma, self.dz, self.dgamma, self.dbeta, self.workspace)
         self.steps += 1

@@ -89,3 +89,25 @@ def test_the_loss_divides_by_the_rows_that_have_a_class(calls):
     loss.forward(torch.zeros(20, 4), torch.zeros(20, dtype=torch.int32))
     loss.backward(torch.zeros(20, 4), torch.zeros(20, dtype=torch.int32), 8)
     assert calls[-1][0] == "adaqp_logprob_backward" and calls[-1][1][7] == -1.0 / 8
+
+
+def test_backward_drops_what_forward_dropped_though_the_share_has_changed_since(calls):
+    x, dy = torch.zeros(20, 8), torch.zeros(20, 8)
+
+    def shares():
+        found = [args[2] for name, args in calls if name == "adaqp_dropout"]
+        calls.clear()
+        return found
+    layer = DenseLayer(20, 8, 8, "cpu", drop=0.5)
+    layer.forward(x)
+    layer.drop = 0.25
+    layer.backward(dy)
+    assert shares() == [0.5, 0.5]
+    layer.forward(x)
+    layer.drop = 0.0
+    layer.backward(dy)
+    assert shares() == [0.25, 0.25]
+    layer.forward(x)
+    layer.drop = 0.5
+    layer.backward(dy)
+    assert shares() == []
