@@ -7,7 +7,7 @@
 // The largest logits are kept by a wave: a list in the LDS, and the n_top-th so far.  Only what is above that is added to the list, and the list is cut back to n_top
 // when it is full: each of its members counts those above it.
 //
-// Bound by memory, and with many classes by the vector instructions nearly as much (11 a logit, one of them an exponential at a quarter of the rate).  Measured: 58 000 x 41 fp32 6.9 us, its gradient 7.3; 4096 x 32 001 bf16 54 us
+// Bound by memory, and with many classes by the vector instructions nearly as much (12 a logit, one of them an exponential at a quarter of the rate).  Measured: 58 000 x 41 fp32 6.9 us, its gradient 7.3; 4096 x 32 001 bf16 54 us
 // (262 MB, 4.9 TB/s; with a branch for a new largest 95), its gradient 85 (524 MB, 6.1 TB/s, in part from the last cache); 65 536 x 1000 fp32 44 us (5.9 TB/s).  3 x 128 000 bf16 with the 20 likeliest 11.6 us, and 5.1 for
 // joining 31 splits of a row: waits, of the cuts of three lists after one another.
 #include "adaqp_train.h"
@@ -16,7 +16,7 @@
 namespace adaqp {
 namespace {
 
-constexpr float kLog2E = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLog2E = 1.4426950408889634f;
 constexpr int kMostTop = ADAQP_LOGPROB_MOST_TOP;
 constexpr float kNothing = -200.0f;                 // exp of it is 0 in fp32
 
@@ -50,15 +50,15 @@ __device__ __forceinline__ Part join(const Part &a, const Part &b)
 }
 
 // A lane's logits as they come: of the largest so far and the next, the smaller is counted and the larger kept, so that the largest of all is never counted.  Sums are in units of
-// exp(base), a logit that the lane has seen; it moves where they could grow out of fp32.  In powers of two, y = x log2(e) - base log2(e), one fma: what the rounding of its last term
-// does to all terms alike is taken back at the end (`off`).
+// exp(base), a logit that the lane has seen; it moves where they could grow out of fp32.  The difference from base comes before the product with log2(e): it is exact for logits near base however large
+// both are, where in fma(x, log2(e), -base log2(e)) the last term's rounding, 2^-24 of |base|, passes the exponents of fp32 from 5e9 on (logits that are masked by a finite number).
 struct Running {
-    float base, shift, max, others, moment;         // shift = - base log2(e)
+    float base, max, others, moment;
 
     __device__ __forceinline__ void begin()
     {
         base = max = -__builtin_inff();
-        shift = others = moment = 0.0f;
+        others = moment = 0.0f;
     }
 
     // N logits, not all of which need be there (those are -inf); the largest of them.
@@ -71,12 +71,11 @@ struct Running {
         if (!(most <= base + 30.0f)) {              // the lane's first, NaN, or far above
             const Part p = part();
             base = most;
-            shift = -base * kLog2E;
             others = moment = 0.0f;
             if (is_part(p)) {
-                const float down = p.max - base, e = exp_of(down), clamped = fmaxf(down, kNothing) * kLog2E;
+                const float down = p.max - base, e = exp_of(down), clamped = fmaxf(down, kNothing);
                 others = p.others * e;
-                moment = p.moment * kLog2E * e + clamped * others;
+                moment = p.moment * e + clamped * others;
             }
         }
         if (base == -__builtin_inff()) return most; // all are
@@ -84,9 +83,9 @@ struct Running {
         for (int k = 0; k < N; ++k) {
             const float low = __builtin_elementwise_minimum(max, x[k]);
             max = __builtin_elementwise_maximum(max, x[k]);
-            const float y = __builtin_elementwise_maximum(__builtin_fmaf(low, kLog2E, shift), kNothing * kLog2E), e = __builtin_amdgcn_exp2f(y);
+            const float u = __builtin_elementwise_maximum(low - base, kNothing), e = exp_of(u);
             others += e;
-            moment = __builtin_fmaf(y, e, moment);
+            moment = __builtin_fmaf(u, e, moment);
         }
         return most;
     }
@@ -94,9 +93,8 @@ struct Running {
     __device__ __forceinline__ Part part() const
     {
         if (max == -__builtin_inff()) return no_part();
-        const float off = (float)(-(double)base * (double)kLog2E - (double)shift);
-        const float down = base - max, e = exp_of(down), sum = others * (e * __builtin_amdgcn_exp2f(off));
-        return Part{max, sum, __builtin_fmaf(__builtin_fmaf(off, kLn2, fmaxf(down, kNothing)), sum, moment * kLn2 * (e * __builtin_amdgcn_exp2f(off)))};
+        const float down = base - max, e = exp_of(down), sum = others * e;
+        return Part{max, sum, __builtin_fmaf(fmaxf(down, kNothing), sum, moment * e)};
     }
 };
 
