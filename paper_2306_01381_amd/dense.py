@@ -187,8 +187,10 @@ class ClassLoss:
         return self.logp
 
     def backward(self, logits: torch.Tensor, targets: torch.Tensor, n_given: int) -> torch.Tensor:
-        """The logits' gradient of -sum(logp) / n_given, after forward() of the same."""
-        B.adaqp_logprob_backward(logits, self.n_classes, targets, self.stats, None, None, None, -1.0 / n_given, self.dlogits)
+        """The logits' gradient of -sum(logp) / n_given, after forward() of the same.  n_given: rows whose target is a class; with 0, the sum of no row, the gradient is zeros."""
+        if n_given < 0:
+            raise ValueError(f"{n_given} rows cannot have a class")
+        B.adaqp_logprob_backward(logits, self.n_classes, targets, self.stats, None, None, None, -1.0 / n_given if n_given else 0.0, self.dlogits)
         return self.dlogits
 
     def likeliest(self, logits: torch.Tensor, n: int):

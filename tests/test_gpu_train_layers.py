@@ -116,6 +116,14 @@ def test_class_loss():
     assert np.array_equal(classes.cpu().numpy(), O.largest(_np(logits), 3)) and np.allclose(_np(top), np.take_along_axis(logp, O.largest(_np(logits), 3), 1), atol=1e-5)
 
 
+def test_class_loss_without_given_classes():
+    """A batch none of whose rows has a class: no log probability and no slope."""
+    logits, none = torch.randn(70, 47, device=DEV), torch.full((70,), -1, dtype=torch.int32, device=DEV)
+    loss = ClassLoss(70, 47, DEV)
+    loss.dlogits.fill_(-77.0)
+    assert not loss.forward(logits, none).any() and not loss.backward(logits, none, 0).any()
+
+
 def _example():
     path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "train_nodes.py")
     spec = importlib.util.spec_from_file_location("train_nodes", path)

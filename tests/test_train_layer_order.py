@@ -111,3 +111,14 @@ def test_backward_drops_what_forward_dropped_though_the_share_has_changed_since(
     layer.drop = 0.5
     layer.backward(dy)
     assert shares() == []
+
+
+def test_the_loss_of_a_batch_without_given_classes_has_no_slope(calls):
+    loss, logits, none = ClassLoss(20, 4, "cpu"), torch.zeros(20, 4), torch.full((20,), -1, dtype=torch.int32)
+    loss.forward(logits, none)
+    assert loss.backward(logits, none, 0) is loss.dlogits
+    assert calls[-1][0] == "adaqp_logprob_backward" and calls[-1][1][7] == 0.0
+    before = len(calls)
+    with pytest.raises(ValueError):
+        loss.backward(logits, none, -1)
+    assert len(calls) == before
