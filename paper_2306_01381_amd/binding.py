@@ -1234,7 +1234,9 @@ def adaqp_f8_matmul_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def adaqp_f8_matmul(a: Tuple[torch.Tensor, torch.Tensor], b: Tuple[torch.Tensor, torch.Tensor], k: int, out: torch.Tensor,
                     workspace: Optional[torch.Tensor], stream: Optional[torch.cuda.Stream] = None) -> None:
-    """out = a b^T for 8-bit matrices of k columns.  out: rows that are whole 128-byte lines are written to their last line's end, zeros behind b's last row's column."""
+    """out = a b^T for 8-bit matrices of k columns.  out: rows that are whole 128-byte lines are written to their last line's end, zeros behind b's last row's column.  fp32 outputs, and those of at most 32
+    rows, are sums of exact products in fp32; bf16 outputs of more rows come from the faster instructions that keep 14 bits of every eight columns' products, so that a row's last bits may change where the
+    batch passes 32 rows."""
     ac, asc, m = _f8(a, None, k, "a")
     bc, bsc, n = _f8(b, None, k, "b")
     op, rows, ldo, kind = _cells(out, n, "out")

@@ -1,7 +1,7 @@
 // Dropout (adaqp_train.h): y = add + keep * x / (1 - p), the choices from a counter-based generator.
 //
-// A lane has pieces of 8 columns: one Philox call, whose 128 bits are their 16-bit numbers.  Nothing is stored of the choices.  Bound by memory: 5 instructions of an element are the
-// generator's and about 4 the rest, hidden behind 8 bytes of fp32 and, less far, 4 of bf16.  Measured: 376 000 x 256 bf16 with a residual 104 us (578 MB, 5.5 TB/s; a copy of 1 GiB runs at 5.2), 2000 x 128 fp32 3.3 us.
+// A lane has pieces of 8 columns: one Philox call, whose 128 bits are their 16-bit numbers.  Nothing is stored of the choices.  Bound by memory: of 20 vector
+// instructions an element (bf16, with a residual) 5 are the generator's; they keep the units busy in 47 % of the cycles.  Measured: 376 000 x 256 bf16 with a residual 104 us (578 MB, 5.5 TB/s; a copy of 1 GiB runs at 5.2), 2000 x 128 fp32 3.3 us.
 #include "adaqp_train.h"
 #include "philox.hpp"
 #include "rows.hpp"

@@ -11,7 +11,8 @@
 // Gradient: the sorted places are cut into chunks.  A group of lanes walks a chunk, adds the rows of equal ids in registers and stores the sum of every run that lies in
 // its chunk; of the runs that go on it leaves the parts (the first run's as the chunk's head, the last one's as its tail), and a second kernel adds a tail and the heads
 // behind it; where entries have very many ids each one between them adds heads by blocks of 64.  Entries without a row are found by a search of the sorted ids, 64 places a step, and set to zero beside it in the same launch.  Bound by memory: 131 072 ids, 50 000 x 1024 fp32, 142 us (742 MB, 5.2 TB/s; 178 where the
-// gradient's rows, which are read once, go through the caches) and 14 for the second kernel, whose longest run has 380 heads; 9001 ids, 20 000 x 301 bf16, 10.7 and 5 us, a chain of waits.
+// gradient's rows, which are read once, go through the caches) and 14 for the second kernel, whose longest run has 380 heads; 9001 ids, 20 000 x 301 bf16, 10.7 and 5 us, a chain of waits.  Added to the table instead,
+// both launches: 148 us (147 whole) and 17 (18); 306 000 ids of 456 000 x 64, a fifth of them named, 54 (68: the others are not set to zero); 58 000 x 256, each named once, 44 (30: the table is read, too).
 #include "adaqp_train.h"
 #include "rows.hpp"
 
@@ -444,7 +445,6 @@ __device__ __forceinline__ void places_below(const int32_t *sorted, int64_t n, i
 }
 
 // Zeros in the entries of a wave's a.clear, at most 64, that no id names.
-
 __device__ __forceinline__ void clear_entries(const GradArgs &a, int64_t tile, uint8_t *named)
 {
     const int lane = threadIdx.x % kWave;
@@ -493,8 +493,7 @@ __global__ __launch_bounds__(kBlock) void embedding_runs_kernel(GradArgs a)
     if (chunk < a.chunks) walk_chunk<T, LANES, V, CHUNK, ONCE>(a, chunk, (int32_t)(slab * LANES + threadIdx.x % LANES) * V);       // lanes behind the columns, too: they hold ids
 }
 
-// Of chunks [kBlockChunks b, kBlockChunks (b + 1)) that all begin inside the same run, the sum of their heads: few ids with very many places each would leave the next kernel thousands of heads to add in turn.
-constexpr int kBlockChunks = 64;
+constexpr int kBlockChunks = 64;                    // chunks whose heads are added together where one run covers them all
 
 constexpr int kJoinWaves = 8, kJoinCols = kWave * 4, kFewHeads = 16;
 
@@ -517,6 +516,7 @@ __device__ __forceinline__ void add_rows(const float *from, int64_t pitch, int64
     }
 }
 
+// Of chunks [kBlockChunks b, kBlockChunks (b + 1)) that all begin inside the same run, the sum of their heads: few ids with very many places each would leave the next kernel thousands of heads to add in turn.
 __global__ __launch_bounds__(kJoinWaves * kWave) void embedding_blocks_kernel(GradArgs a)
 {
     __shared__ float part[kJoinWaves][kJoinCols];
@@ -634,7 +634,8 @@ int64_t grad_pitch(int32_t dim) { return ((int64_t)dim + 7) / 8 * 8; }
 int64_t grad_blocks(int64_t n_ids, int32_t dim) { return grad_chunks(n_ids, dim) < 2048 ? 0 : grad_chunks(n_ids, dim) / kBlockChunks; }
 
 // Ids for each entry from which on the blocks have a launch of their own: the places of a block.  Without and with, fp32: 65 536 ids of 10 entries x 256 53 and 37 us, 131 072 of 40 x 1024
-// 113 and 111; of 256 x 1024 110 and 113, of 50 000 x 1024 147 and 153.  A large table with one very frequent id has none: the host does not know the ids.
+// 113 and 111; of 256 x 1024 110 and 113, of 50 000 x 1024 147 and 153.  A large table with one very frequent id has none, since the host does not know the ids, and waits for the workgroups that add its
+// heads: where one of 50 000 entries has half of the ids, 131 072 ids x 1024 take 166 (151 without it), 306 000 x 256 147 (87), 306 000 x 64 106 (41).  An id that stands for no entry is better outside the table.
 constexpr int64_t kManyPlaces = kBlockChunks * kLongChunk;
 
 template <typename T, int LANES>

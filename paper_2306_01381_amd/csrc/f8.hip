@@ -2,7 +2,7 @@
 //
 // 16 lanes hold the 128 columns of a block, 8 neighbouring ones each.  Where only the rows' form with a scale for each row is wanted the blocks of all rows are dealt out in a row; else a
 // workgroup takes a tile of 128 columns and 128 rows in registers.  x is read once.  Bound by memory.  Measured: 58 000 x 602 fp32 rows 27 us (176 MB, 6.5 TB/s, in part from the last cache), both forms 40 us (5.2 TB/s; 68 with fp32 values
-// turned in the LDS, of which two workgroups fit a CU); 179 000 x 300 bf16 rows 30 us, read back 28 us (5.7 TB/s).
+// turned in the LDS, of which two workgroups fit a CU), on operands that no cache holds 33 and 45; with a scale for a tile 36 and 44; 179 000 x 300 bf16 rows 30 us, read back 28 us (5.7 TB/s).
 #include "f8.hpp"
 #include "rows.hpp"
 

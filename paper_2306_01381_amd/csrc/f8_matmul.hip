@@ -12,8 +12,9 @@
 // Where the tiles are few, k is split over workgroups; the parts' sums, fp32, are added in order by a second kernel.  With at most 32 rows nothing is used
 // twice but those: a workgroup takes 32 columns of out, its eight waves share the lines of k and read them into registers.
 //
-// What bounds it: large products the matrix cores and power.  8192 x 8192 x 4096, bf16 out, takes 227 to 250 us (2.2 to 2.4 PFLOP/s; zeros, which draw less, 182); of a tile's 57 us its first loads and its stores take 6, with the
-// matrix cores idle.  With fp32 outputs 425 us, 1.3 PFLOP/s, what a library's bf16 product reaches on this card (1.2).  Shallow products the output: 179 000 x 256, k = 300, bf16 out, 34 us (149 MB, 4.3 TB/s).  Deep ones the operands
+// What bounds it: large products the matrix cores, power and waits.  8192 x 8192 x 4096, bf16 out, takes 227 to 254 us (2.2 to 2.4 PFLOP/s; zeros, which draw less, 182); the matrix cores are busy in 54 % of the cycles, at a clock that falls
+// to 1.9 GHz; of a tile's 57 us its first loads and its stores take 6, with the matrix cores idle.  With fp32 outputs 425 to 465 us, 1.2 to 1.3 PFLOP/s, what a library's bf16 product reaches on this card (1.2); the matrix cores are
+// busy in 63 % of the cycles, the vector units, for the most part with conversions, in 31 %.  Shallow products the output: 179 000 x 256, k = 300, bf16 out, 34 us (149 MB, 4.3 TB/s).  Deep ones the operands
 // and the conversions: 256 x 602, k = 58 000, fp32 out, 26 us and 5 to add up the parts.  Few rows their waits: 5 x 8192, k = 4096, 8 us (34 MB, 4.2 TB/s).
 #include "f8.hpp"
 #include "lines.hpp"

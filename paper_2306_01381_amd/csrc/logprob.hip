@@ -7,8 +7,9 @@
 // The largest logits are kept by a wave: a list in the LDS, and the n_top-th so far.  Only what is above that is added to the list, and the list is cut back to n_top
 // when it is full: each of its members counts those above it.
 //
-// Bound by memory, and with many classes by the vector instructions nearly as much (12 a logit, one of them an exponential at a quarter of the rate).  Measured: 58 000 x 41 fp32 6.9 us, its gradient 7.3; 4096 x 32 001 bf16 54 us
-// (262 MB, 4.9 TB/s; with a branch for a new largest 95), its gradient 85 (524 MB, 6.1 TB/s, in part from the last cache); 65 536 x 1000 fp32 44 us (5.9 TB/s).  3 x 128 000 bf16 with the 20 likeliest 11.6 us, and 5.1 for
+// Bound by memory, and with many classes in 16 bits by the vector instructions as much: 13 a logit, one of them an exponential at a quarter of the rate, and 26 in the gradient.  Measured: 58 000 x 41 fp32 6.8 us, its gradient 7.3;
+// 4096 x 32 001 bf16 63 us on operands that the caches do not hold (262 MB, 4.2 TB/s, the vector units busy in 74 % of the cycles; 53 to 59 where a part is in the last cache; with a branch for a new largest 95), its gradient 88
+// (524 MB, 6.0 TB/s, in part from the last cache, the vector units always busy); 65 536 x 1000 fp32 44 us (5.9 TB/s).  3 x 128 000 bf16 with the 20 likeliest 11.6 us, and 5.1 for
 // joining 31 splits of a row: waits, of the cuts of three lists after one another.
 #include "adaqp_train.h"
 #include "rows.hpp"
@@ -389,7 +390,6 @@ __global__ __launch_bounds__(WAVES * kWave) void logprob_kernel(ProbArgs a)
     if (TOP && lane < a.n_top) a.places[(row * a.splits + split) * a.n_top + lane] = lane < largest.count ? lists[0][lane] : 0;
 }
 
-// Rows of at most 64 lanes' registers: LANES lanes have one, PIECES pieces of 8 logits each.
 template <int LANES>
 __device__ __forceinline__ Place lane_most(Place v)
 {
@@ -401,6 +401,7 @@ __device__ __forceinline__ Place lane_most(Place v)
     return v;
 }
 
+// Rows of at most 64 lanes' registers: LANES lanes have one, PIECES pieces of 8 logits each.
 template <typename T, int LANES, int PIECES, int EACH, bool TOP>
 __global__ __launch_bounds__(kBlock) void logprob_rows_kernel(ProbArgs a)
 {
@@ -586,8 +587,8 @@ template <typename T, bool ONCE>
 __global__ __launch_bounds__(kBlock) void logprob_gradient_kernel(ProbGradArgs a)
 {
     constexpr int kEach = 2;
-    // From the last row to the first, and stored past the caches where the logits fill them: what the forward pass read last is still there.  4096 x 32 001 bf16, both passes: 169 us, from the first
-    // row on 176, stored through the caches 188.
+    // From the last row to the first, and stored past the caches where the logits fill them: what the forward pass read last is still there.  4096 x 32 001 bf16, both passes on the same logits 138 us,
+    // from the first row on 142, stored through the caches 168; on others each time 151, 152, 171.
     const uint64_t first = (uint64_t)(workgroups() - 1 - workgroup()) * (kBlock * kEach) + threadIdx.x;
     int64_t row[kEach];
     int32_t col[kEach];
